@@ -1,0 +1,129 @@
+/*
+ * foe_cache.h -- paged KV cache held in 8 bits: writing it, attention over it, eviction from it, and the forward pass of
+ * a layer (foe.h) on it.
+ *
+ * The cache.  Pages of 64 tokens.  K and V are codes of 8 bits, and the codes of one page and KV head share one fp32
+ * scale: a code c stands for c * scale.  FOE_CACHE_E4M3: c is an e4m3 number (largest magnitude 448).  FOE_CACHE_INT8: c
+ * is an integer in [-127, 127].  Scales are powers of two, 2^e with the smallest e in [-32, 64] for which the page's rows
+ * of that head fit (largest magnitude <= 448 or 127 times the scale); dividing by one is exact, so a code is ONE rounding
+ * (nearest, ties to even) of the bf16 value, off by at most half a step of its format.
+ *   - A page that already holds rows keeps the larger of its exponent and the one the new rows need; if it grows, the
+ *     held codes are rounded again at the new scale (for e4m3 this only changes codes that become subnormal).
+ *   - Rows with an infinity, a NaN or a magnitude above 2^64 times the largest code make the scale of their page and head
+ *     NaN, and every attention output that reads it is NaN, until the page is written again from its first row.
+ *   - Rows of a page behind its last token are neither read into a result nor written.
+ *
+ * The handle (foe_cache) holds the shapes and the workspace; pages, scales and tables belong to the caller and are named
+ * in a foe_cache_view on every call.  The conventions of foe.h hold: device pointers, asynchronous calls on the given
+ * stream, one stream at a time per handle, the same inputs give the same bits, argument checks before anything is
+ * launched, device-side conditions in a status word (foe_cache_poll_status).  Calls only launch kernels, so they can be
+ * captured into a CUDA graph; graphs captured from one handle share its workspace and must not run at the same time.
+ * A handle belongs to the device that was current when it was created; calls with another device current are refused
+ * (FOE_ERR_UNSUPPORTED).
+ */
+#ifndef FOE_CACHE_H_
+#define FOE_CACHE_H_
+
+#include "foe.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef enum { FOE_CACHE_E4M3 = 0, FOE_CACHE_INT8 = 1 } foe_cache_format;
+
+/* Validity: n_q_heads % n_kv_heads == 0, n_q_heads / n_kv_heads <= 16, head_dim in {64, 96, 128}, page_size == 64,
+ * max_* > 0, max_seqs <= 65535, n_kv_heads <= 65535. */
+typedef struct {
+  int n_q_heads, n_kv_heads, head_dim;
+  int page_size;
+  int format;              /* foe_cache_format */
+  int max_tokens;          /* largest n_tokens of a call with q_lens */
+  int max_seqs;            /* largest n_seqs of any call */
+  int max_context;         /* largest number of tokens a sequence holds, the new ones of a call included */
+  int track_weights;       /* nonzero: foe_cache_attend may be asked for weights (workspace of
+                              max_seqs * n_q_heads * max_context fp32) */
+  int for_layers;          /* nonzero: foe_cache_block may be called (staging of max_tokens K and V rows) */
+} foe_cache_config;
+
+/* One call's view of the cache (device pointers; the struct itself is in host memory). */
+typedef struct {
+  void* k_pages;           /* [num_pages][n_kv_heads][64][head_dim] codes, 16-byte aligned */
+  void* v_pages;
+  float* k_scales;         /* [num_pages][n_kv_heads] */
+  float* v_scales;
+  const int* block_table;  /* [n_seqs][max_pages_per_seq] physical page ids */
+  const int* context_lens; /* [n_seqs] tokens cached before the call */
+  const int* q_lens;       /* [n_seqs] new tokens of the call; NULL: one each */
+  const int* positions;    /* [n_seqs] position (for RoPE) of a sequence's first new token, or NULL: context_lens.  Only
+                              foe_cache_block reads it; after an eviction a sequence holds fewer tokens than it has seen */
+  int n_seqs, max_pages_per_seq, num_pages;
+  int n_tokens;            /* host copy of sum(q_lens) (ignored with q_lens == NULL) */
+  int max_q_len;           /* host upper bound of q_lens (ignored with q_lens == NULL) */
+} foe_cache_view;
+
+typedef struct foe_cache foe_cache;
+
+/* Allocates the workspace.  *out receives the handle. */
+foe_status foe_cache_create(const foe_cache_config* config, foe_cache** out);
+
+/* Frees everything the handle owns.  NULL is accepted. */
+foe_status foe_cache_destroy(foe_cache* cache);
+
+/* Writes the K and V rows of the call's new tokens (the sequences' tokens concatenated in order) at logical positions
+ * context_lens[s] .. context_lens[s] + q_len - 1.  k, v: bf16, row t at k + t * k_stride elements, [n_kv_heads][head_dim]
+ * contiguous inside a row (K after RoPE); strides at least n_kv_heads * head_dim and multiples of 8.  Pages that the call
+ * writes belong to one sequence of the call; context_lens is not changed.
+ * Errors: FOE_ERR_NULL, FOE_ERR_SHAPE (sizes, strides, alignment); n_tokens == 0 or n_seqs == 0 is FOE_OK, no work. */
+foe_status foe_cache_append(foe_cache* cache, const void* k, long long k_stride, const void* v, long long v_stride,
+                            const foe_cache_view* view, void* stream);
+
+/* out = causal softmax(q k^T / sqrt(head_dim)) v of the call's new tokens over the cached and the new tokens (which
+ * foe_cache_append has written): query i of sequence s sees the keys 0 .. context_lens[s] + i.  q, out: bf16, row t at
+ * t * stride elements, [n_q_heads][head_dim] inside a row; strides at least n_q_heads * head_dim and multiples of 8; out
+ * must not alias q.  Query head a reads KV head a / (n_q_heads / n_kv_heads).
+ * With weights (both pointers or neither; fp32 [n_seqs][n_kv_heads], row stride weights_stride >= the smaller of
+ * 64 * max_pages_per_seq and max_context):
+ *     weights_out[s][h][j] = weights_in[s][h][j] + sum of the probabilities of key j
+ * over the query heads of KV head h and the last `window` queries of the sequence (0: all of them), for every key j the
+ * sequence holds; entries behind are left as they were.  weights_in may be weights_out.  Sequences without new tokens
+ * keep weights_in as it is. */
+foe_status foe_cache_attend(foe_cache* cache, const void* q, long long q_stride, const foe_cache_view* view, void* out,
+                            long long out_stride, const float* weights_in, float* weights_out, long long weights_stride,
+                            int window, void* stream);
+
+/* Cuts every sequence of the view (context_lens = tokens it holds; q_lens is not read) to at most `budget` tokens, for
+ * each KV head by itself: the first `sink` tokens, the last `recent` ones and of the others those with the largest
+ * weights (equal weights: the lower position; a NaN is below every number) are kept, in their order; a sequence within the
+ * budget keeps everything.  The kept rows are copied into the pages to_table [n_seqs][to_pages_per_seq] of the same pool,
+ * whose scales are made anew from them; the pages the view names are not changed, so a page that sequences share can be a
+ * source for all of them.  The pages of to_table are distinct and none of them is named by the view.
+ * Results: new_lens [n_seqs] = min(tokens, budget); kept [n_seqs][n_kv_heads][budget] the kept positions; weights_out (or
+ * NULL) [n_seqs][n_kv_heads], row stride weights_out_stride >= budget, the weights of the kept tokens, which must not
+ * alias weights.  Entries and rows behind new_lens are left as they were.
+ * 0 <= sink, 0 <= recent, sink + recent <= budget, 64 * to_pages_per_seq >= budget >= 1 (FOE_ERR_SHAPE otherwise). */
+foe_status foe_cache_evict(foe_cache* cache, const foe_cache_view* view, const float* weights, long long weights_stride,
+                           const int* to_table, int to_pages_per_seq, int budget, int sink, int recent, int* new_lens,
+                           int* kept, float* weights_out, long long weights_out_stride, void* stream);
+
+/* foe_prefill (decode == 0; q_lens given) or foe_decode (decode != 0; q_lens NULL) of `layer` with its K and V in this
+ * cache: the QKV projection, foe_cache_append, foe_cache_attend and the rest of the block, x and out as there.  The layer
+ * and the handle agree in n_q_heads, n_kv_heads and head_dim (FOE_ERR_CONFIG otherwise); weights as in foe_cache_attend.
+ * Device-side conditions are reported by foe_poll_status of the layer. */
+foe_status foe_cache_block(foe_layer* layer, foe_cache* cache, const void* x, const foe_cache_view* view, void* out,
+                           const float* weights_in, float* weights_out, long long weights_stride, int window, int decode,
+                           void* stream);
+
+/* Synchronises the handle's last stream and reads the device status word into *device_status (FOE_OK, FOE_ERR_TIMEOUT or
+ * FOE_ERR_BOUNDS: a page id outside the pool, or lengths that exceed the table, max_context, max_q_len or n_tokens; what
+ * belongs to such a sequence or page is skipped); the word is reset to FOE_OK afterwards. */
+foe_status foe_cache_poll_status(foe_cache* cache, int* device_status);
+
+/* Host-only, no device work: what the checks of a handle created with `config` say to a view (FOE_OK, or the error that a
+ * call with it returns before anything is launched). */
+foe_status foe_cache_check(const foe_cache_config* config, const foe_cache_view* view);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* FOE_CACHE_H_ */

@@ -8,7 +8,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfoe.so")
-SOURCES = ["foe_api.cu", "gemm_tcgen05.cu", "attention.cu", "attention_tc.cu", "smallm.cu", "route.cu", "router_tc.cu", "permute.cu", "elementwise.cu", "shard.cu", "decode_proj.cu"]
+SOURCES = ["foe_api.cu", "gemm_tcgen05.cu", "attention.cu", "attention_tc.cu", "smallm.cu", "route.cu", "router_tc.cu", "permute.cu", "elementwise.cu", "shard.cu", "decode_proj.cu",
+           "cache8_api.cu", "cache8_append.cu", "cache8_attention.cu", "cache8_attention_tc.cu", "cache8_weights.cu", "cache8_evict.cu"]
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC",
          "-cudart", "static"]
 
@@ -18,6 +19,7 @@ def _stale() -> bool:
         return True
     t = os.path.getmtime(LIB)
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(HERE, "..", "include", "foe.h"), os.path.join(HERE, "..", "include", "foe_shard.h"),
+                                                                 os.path.join(HERE, "..", "include", "foe_cache.h"),
                                                                  os.path.abspath(__file__)]
     return any(os.path.getmtime(p) > t for p in deps)
 

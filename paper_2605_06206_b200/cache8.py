@@ -1,0 +1,241 @@
+"""The paged KV cache in 8 bits (include/foe_cache.h): thin ctypes binding, argument marshalling only.
+
+    ops = CacheOps(shape, "e4m3", max_tokens, max_seqs, max_context)      # shapes and workspace
+    cache = empty_cache(shape, "e4m3", num_pages)                          # codes and scales, owned by the caller
+    view = cache.view(block_table, context_lens, q_lens)                   # one call's view (q_lens None: one token each)
+    ops.append(k, v, view)                                                 # quantise and write the new tokens' rows
+    out = ops.attend(q, view)                                              # attention over cached and new tokens
+    ops.evict(view, weights, to_table, budget, sink, recent, ...)          # cut every sequence to its heaviest tokens
+    out = ops.block(layer, x, view)                                        # a layer's forward pass on this cache
+
+There is no fallback: if the library is missing or no CUDA device is present the calls raise.
+"""
+from __future__ import annotations
+
+import ctypes
+import dataclasses
+from typing import Optional
+
+import torch
+
+from . import binding
+from .binding import _check, _ptr
+
+FORMATS = {"e4m3": 0, "int8": 1}
+LARGEST = {"e4m3": 448.0, "int8": 127.0}
+PAGE = 64
+CACHE_EXPORTS = ["foe_cache_create", "foe_cache_destroy", "foe_cache_append", "foe_cache_attend", "foe_cache_evict",
+                 "foe_cache_block", "foe_cache_poll_status", "foe_cache_check"]
+
+
+class FoeCacheConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in
+                ("n_q_heads", "n_kv_heads", "head_dim", "page_size", "format", "max_tokens", "max_seqs", "max_context",
+                 "track_weights", "for_layers")]
+
+
+class FoeCacheView(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in
+                ("k_pages", "v_pages", "k_scales", "v_scales", "block_table", "context_lens", "q_lens", "positions")] + \
+               [(n, ctypes.c_int) for n in ("n_seqs", "max_pages_per_seq", "num_pages", "n_tokens", "max_q_len")]
+
+
+_declared = False
+
+
+def load_library() -> ctypes.CDLL:
+    """libfoe.so with the prototypes of include/foe_cache.h declared."""
+    global _declared
+    lib = binding.load_library()
+    if not _declared:
+        vp, ci, ll = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong
+        view = ctypes.POINTER(FoeCacheView)
+        lib.foe_cache_create.argtypes = [ctypes.POINTER(FoeCacheConfig), ctypes.POINTER(vp)]
+        lib.foe_cache_destroy.argtypes = [vp]
+        lib.foe_cache_append.argtypes = [vp, vp, ll, vp, ll, view, vp]
+        lib.foe_cache_attend.argtypes = [vp, vp, ll, view, vp, ll, vp, vp, ll, ci, vp]
+        lib.foe_cache_evict.argtypes = [vp, view, vp, ll, vp, ci, ci, ci, ci, vp, vp, vp, ll, vp]
+        lib.foe_cache_block.argtypes = [vp, vp, vp, view, vp, vp, vp, ll, ci, ci, vp]
+        lib.foe_cache_poll_status.argtypes = [vp, ctypes.POINTER(ci)]
+        lib.foe_cache_check.argtypes = [ctypes.POINTER(FoeCacheConfig), view]
+        for name in CACHE_EXPORTS:
+            getattr(lib, name).restype = ci
+        _declared = True
+    return lib
+
+
+@dataclasses.dataclass(frozen=True, eq=False)
+class Paged8:
+    """One call's view of an 8-bit cache.  Checked and described to the library once, when it is made: a decode loop keeps
+    its view and changes the lengths on the device (foe_context_advance)."""
+    k_pages: torch.Tensor                 # [num_pages, n_kv, 64, dh] uint8 codes
+    v_pages: torch.Tensor
+    k_scales: torch.Tensor                # [num_pages, n_kv] fp32, powers of two
+    v_scales: torch.Tensor
+    block_table: torch.Tensor             # [n_seqs, max_pages_per_seq] int32
+    context_lens: torch.Tensor            # [n_seqs] int32, tokens cached before the call
+    q_lens: Optional[torch.Tensor] = None     # [n_seqs] int32 new tokens; None: one each
+    positions: Optional[torch.Tensor] = None  # [n_seqs] int32 RoPE position of the first new token; None: context_lens
+
+    def __post_init__(self):
+        pages, n_kv, page, dh = self.k_pages.shape
+        pool = (self.k_pages, self.v_pages, self.k_scales, self.v_scales)
+        lens = (self.block_table, self.context_lens, self.q_lens, self.positions)
+        for t in pool + lens:
+            assert t is None or (t.is_contiguous() and t.device == self.k_pages.device)
+        assert page == PAGE and self.v_pages.shape == self.k_pages.shape
+        assert self.k_pages.element_size() == 1 and self.v_pages.element_size() == 1
+        for t in pool[2:]:
+            assert t.shape == (pages, n_kv) and t.dtype == torch.float32
+        n, width = self.block_table.shape
+        for t in lens:
+            assert t is None or (t.dtype == torch.int32 and t.shape[0] == n)
+        c = FoeCacheView(*[t.data_ptr() for t in pool], *[_ptr(t) for t in lens], n, width, pages, n, 1)
+        for name, v in (("c", c), ("n_seqs", n), ("dims", (n_kv, dh)), ("device_index", self.k_pages.get_device())):
+            object.__setattr__(self, name, v)
+
+
+@dataclasses.dataclass
+class Pool8:
+    """Codes and scales of a pool of pages."""
+    k_pages: torch.Tensor
+    v_pages: torch.Tensor
+    k_scales: torch.Tensor
+    v_scales: torch.Tensor
+
+    def view(self, block_table, context_lens, q_lens=None, positions=None) -> Paged8:
+        return Paged8(self.k_pages, self.v_pages, self.k_scales, self.v_scales, block_table, context_lens, q_lens, positions)
+
+
+def empty_cache(shape, num_pages: int, device: str = "cuda") -> Pool8:
+    """A pool of `num_pages` pages, zeroed (zero codes stand for zeros whatever the format)."""
+    shp = (num_pages, shape.n_kv_heads, PAGE, shape.head_dim)
+    return Pool8(torch.zeros(shp, dtype=torch.uint8, device=device), torch.zeros(shp, dtype=torch.uint8, device=device),
+                 torch.ones(shp[:2], dtype=torch.float32, device=device), torch.ones(shp[:2], dtype=torch.float32, device=device))
+
+
+class CacheOps:
+    """Operators on an 8-bit cache: shapes and workspace (foe_cache_create) on the current CUDA device.
+
+    shape: anything with n_q_heads, n_kv_heads and head_dim (a LayerShape).  weights: whether attend may be asked for
+    accumulated attention weights.  layers: whether block may be called."""
+
+    def __init__(self, shape, fmt: str, max_tokens: int, max_seqs: int, max_context: int, weights: bool = True,
+                 layers: bool = False):
+        if not torch.cuda.is_available():
+            raise RuntimeError("CacheOps needs a CUDA device: the operators have no CPU path")
+        self.lib = load_library()
+        self.n_q, self.n_kv, self.dh, self.fmt = shape.n_q_heads, shape.n_kv_heads, shape.head_dim, fmt
+        cfg = FoeCacheConfig(self.n_q, self.n_kv, self.dh, getattr(shape, "page_size", PAGE), FORMATS[fmt], max_tokens,
+                             max_seqs, max_context, int(weights), int(layers))
+        h = ctypes.c_void_p()
+        _check(self.lib.foe_cache_create(ctypes.byref(cfg), ctypes.byref(h)), "foe_cache_create")
+        self.handle = h
+        self.index = torch.cuda.current_device()
+        self.dims = (self.n_kv, self.dh)
+
+    def close(self) -> None:
+        if getattr(self, "handle", None):
+            self.lib.foe_cache_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    # ---- marshalling helpers
+    def _own(self, *tensors) -> None:
+        for t in tensors:
+            assert t is None or t.get_device() == self.index, f"tensor on {t.device}, operators on cuda:{self.index}"
+
+    def _view(self, v: Paged8, n_tokens: int, max_q_len: Optional[int]):
+        """The view's description, with the call's token counts where it has q_lens."""
+        assert v.dims == self.dims and v.device_index == self.index, "a view of another shape or device"
+        if v.q_lens is None:
+            return v.c
+        if max_q_len is None:
+            max_q_len = int(v.q_lens.max().item()) if v.n_seqs else 0
+        c = FoeCacheView.from_buffer_copy(v.c)
+        c.n_tokens, c.max_q_len = n_tokens, max_q_len
+        return c
+
+    def _rows(self, t: torch.Tensor, heads: int, n: int) -> int:
+        """Row stride of a [n, heads, head_dim] bf16 tensor whose rows are contiguous."""
+        assert t.dtype is torch.bfloat16 and t.get_device() == self.index and t.shape == (n, heads, self.dh)
+        s = t.stride()
+        assert s[2] == 1 and (heads == 1 or s[1] == self.dh), "rows must be contiguous"
+        return s[0] if n > 1 else heads * self.dh
+
+    def _weights(self, view: Paged8, w_in, w_out):
+        if w_in is None and w_out is None:
+            return None, None, 0
+        for w in (w_in, w_out):
+            assert w is not None, "weights_in and weights_out come together"
+            assert w.dtype is torch.float32 and w.is_contiguous() and w.get_device() == self.index
+        shape = w_in.shape
+        assert w_out.shape == shape and len(shape) == 3 and shape[0] == view.n_seqs and shape[1] == self.n_kv
+        return w_in.data_ptr(), w_out.data_ptr(), shape[2]
+
+    def _stream(self, stream) -> int:
+        return torch.cuda.current_stream(self.index).cuda_stream if stream is None else stream.cuda_stream
+
+    # ---- the calls
+    def append(self, k: torch.Tensor, v: torch.Tensor, view: Paged8, max_q_len: Optional[int] = None, stream=None) -> None:
+        """foe_cache_append: k, v [tokens, n_kv, head_dim] bf16 (K after RoPE), any row stride."""
+        n = view.n_seqs if view.q_lens is None else k.shape[0]
+        c = self._view(view, n, max_q_len)
+        _check(self.lib.foe_cache_append(self.handle, k.data_ptr(), self._rows(k, self.n_kv, n), v.data_ptr(),
+                                         self._rows(v, self.n_kv, n), ctypes.byref(c), self._stream(stream)), "foe_cache_append")
+
+    def attend(self, q: torch.Tensor, view: Paged8, out: Optional[torch.Tensor] = None, max_q_len: Optional[int] = None,
+               weights_in: Optional[torch.Tensor] = None, weights_out: Optional[torch.Tensor] = None, window: int = 0,
+               stream=None) -> torch.Tensor:
+        """foe_cache_attend: q [tokens, n_q, head_dim] bf16, any row stride; weights [n_seqs, n_kv, >= longest] fp32."""
+        n = view.n_seqs if view.q_lens is None else q.shape[0]
+        if out is None:
+            out = torch.empty((n, self.n_q, self.dh), dtype=torch.bfloat16, device=f"cuda:{self.index}")
+        c = self._view(view, n, max_q_len)
+        wi, wo, ws = self._weights(view, weights_in, weights_out)
+        _check(self.lib.foe_cache_attend(self.handle, q.data_ptr(), self._rows(q, self.n_q, n), ctypes.byref(c), out.data_ptr(),
+                                         self._rows(out, self.n_q, n), wi, wo, ws, window, self._stream(stream)), "foe_cache_attend")
+        return out
+
+    def evict(self, view: Paged8, weights: torch.Tensor, to_table: torch.Tensor, budget: int, sink: int, recent: int,
+              new_lens: torch.Tensor, kept: torch.Tensor, weights_out: Optional[torch.Tensor] = None, stream=None) -> None:
+        """foe_cache_evict: the kept tokens go to the pages of to_table; new_lens [n_seqs], kept [n_seqs, n_kv, budget]
+        int32 and weights_out [n_seqs, n_kv, >= budget] are written."""
+        n = view.n_seqs
+        self._own(weights, to_table, new_lens, kept, weights_out)
+        for t in (to_table, new_lens, kept):
+            assert t.dtype == torch.int32 and t.is_contiguous() and t.shape[0] == n
+        assert tuple(kept.shape) == (n, self.n_kv, budget) and to_table.dim() == 2
+        for w in (weights, weights_out):
+            assert w is None or (w.dtype == torch.float32 and w.is_contiguous() and tuple(w.shape[:2]) == (n, self.n_kv))
+        c = self._view(view, 0, 0)                       # (q_lens and their sums are not read)
+        _check(self.lib.foe_cache_evict(self.handle, ctypes.byref(c), weights.data_ptr(), weights.shape[2], to_table.data_ptr(),
+                                        to_table.shape[1], budget, sink, recent, new_lens.data_ptr(), kept.data_ptr(),
+                                        _ptr(weights_out), 0 if weights_out is None else weights_out.shape[2],
+                                        self._stream(stream)), "foe_cache_evict")
+
+    def block(self, layer: binding.FoeLayer, x: torch.Tensor, view: Paged8, out: Optional[torch.Tensor] = None,
+              max_q_len: Optional[int] = None, weights_in: Optional[torch.Tensor] = None,
+              weights_out: Optional[torch.Tensor] = None, window: int = 0, stream=None) -> torch.Tensor:
+        """foe_cache_block: layer.prefill (view.q_lens given) or layer.decode with K and V in this cache."""
+        assert x.is_cuda and x.is_contiguous() and x.dtype == torch.bfloat16
+        decode = view.q_lens is None
+        n = view.n_seqs if decode else x.shape[-2]
+        assert x.shape[-2] == n
+        self._own(x)
+        out = layer._out_like(n) if out is None else out
+        c = self._view(view, n, max_q_len)
+        wi, wo, ws = self._weights(view, weights_in, weights_out)
+        _check(self.lib.foe_cache_block(layer.handle, self.handle, x.data_ptr(), ctypes.byref(c), out.data_ptr(), wi, wo, ws,
+                                        window, int(decode), self._stream(stream)), "foe_cache_block")
+        return out
+
+    def poll_status(self) -> int:
+        v = ctypes.c_int(0)
+        _check(self.lib.foe_cache_poll_status(self.handle, ctypes.byref(v)), "foe_cache_poll_status")
+        return v.value

@@ -12,6 +12,7 @@
 #include <math.h>
 
 #include "common.cuh"
+#include "decode_walk.cuh"
 #include "kernels.h"
 
 namespace foe {
@@ -69,86 +70,6 @@ struct DcSmem {
   static constexpr size_t kBytes = size_t(kMiscOff) + 16 + 1024; // + alignment slack
 };
 
-// position inside the list of pages
-struct DcWalk {
-  int b, kvh, page;      // current entry
-  int np, kv_len;        // pages and keys (cached + the new token) of sequence b
-  int seq_first;         // list index of the first page of sequence b
-  int t, t_end;          // current list index, end of this CTA's range
-  int per;
-};
-
-__device__ __forceinline__ int dc_pages(const AttnArgs& a, int b, int* kv_len) {
-  const int ctx = min(max(a.context_lens[b], 0), a.max_kv_pages * 64 - 1);   // (out-of-range values are reported by the QKV step)
-  *kv_len = ctx + 1;                                                          // cached tokens + the new one
-  return (ctx + 64) >> 6;
-}
-
-// Every warp works this out for itself (all 32 lanes): the CTA's range and where it starts.  False: nothing to do.
-__device__ __forceinline__ bool dc_begin(const AttnArgs& a, DcWalk& w) {
-  const int lane = threadIdx.x & 31;
-  int sum = 0, np_first = 0, kl_first = 0;        // (the first 32 sequences' values are kept for the search below)
-  for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
-    int kl = 0;
-    const int np = b0 + lane < a.n_seqs ? dc_pages(a, b0 + lane, &kl) : 0;
-    if (b0 == 0) { np_first = np; kl_first = kl; }
-    sum += np;
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  const int T = sum * a.n_kv;
-  w.per = max(kDcMinTiles, (T + int(gridDim.x) - 1) / int(gridDim.x));
-  const long long t0 = (long long)blockIdx.x * w.per;
-  if (t0 >= T) return false;
-  w.t = int(t0);
-  w.t_end = min(T, w.t + w.per);
-  int base = 0;                                  // pages of the sequences before this chunk of 32
-  for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
-    int kl = kl_first;
-    const int np = b0 == 0 ? np_first : (b0 + lane < a.n_seqs ? dc_pages(a, b0 + lane, &kl) : 0);
-    int incl = np;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += v;
-    }
-    const int first = a.n_kv * (base + incl - np);
-    const bool hit = np > 0 && w.t >= first && w.t < first + a.n_kv * np;
-    const uint32_t m = __ballot_sync(0xffffffffu, hit);
-    if (m) {
-      const int src = __ffs(m) - 1;
-      w.b = b0 + src;
-      w.seq_first = __shfl_sync(0xffffffffu, first, src);
-      w.np = __shfl_sync(0xffffffffu, np, src);
-      w.kv_len = __shfl_sync(0xffffffffu, kl, src);
-      const int rem = w.t - w.seq_first;
-      w.kvh = rem / w.np;
-      w.page = rem - w.kvh * w.np;
-      return true;
-    }
-    base += __shfl_sync(0xffffffffu, incl, 31);
-  }
-  return false;                                  // (not reached: t0 < T)
-}
-
-// pages of the segment that starts at the current entry
-__device__ __forceinline__ int dc_segment_len(const DcWalk& w) { return min(w.np - w.page, w.t_end - w.t); }
-
-__device__ __forceinline__ void dc_advance(const AttnArgs& a, DcWalk& w, int len) {
-  w.t += len;
-  w.page += len;
-  if (w.page >= w.np) {
-    w.page = 0;
-    w.kvh += 1;
-    if (w.kvh == a.n_kv) {
-      w.kvh = 0;
-      w.seq_first += a.n_kv * w.np;
-      w.b += 1;
-      if (w.t < w.t_end) w.np = dc_pages(a, w.b, &w.kv_len);
-    }
-  }
-}
-
 __device__ __forceinline__ void dc_consumer_bar() { asm volatile("bar.sync 1, %0;" ::"n"(kDcConsumers * 32) : "memory"); }
 
 template <int DH>
@@ -178,7 +99,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   // step: it writes q and the new token's K / V, into the last page of every sequence.  Context lengths, the block
   // table and all other pages are older and complete (a kernel lets its successor start only after its own wait).
   DcWalk w;
-  const bool any = dc_begin(a, w);                                 // (warp-uniform, and the same in every warp)
+  const bool any = dc_begin(a, kDcMinTiles, w);                                 // (warp-uniform, and the same in every warp)
 
   if (warp == kDcConsumers) {
     // ------------------------------------------------------------------ producer

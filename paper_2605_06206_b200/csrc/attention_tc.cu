@@ -28,6 +28,7 @@
 // memory is released).
 #include <math.h>
 
+#include "attention_tc.cuh"
 #include "common.cuh"
 #include "kernels.h"
 
@@ -46,48 +47,6 @@ constexpr int kAtThreads = 640;        // warpgroup 0: producer, MMA issuer (+2 
 // back.  The launcher checks the kernel's actual register count against this before the first launch.
 constexpr int kAtRegsLaunch = 96, kAtRegsLow = 32, kAtRegsHigh = 112;
 static_assert(4 * (kAtRegsHigh - kAtRegsLaunch) <= kAtRegsLaunch - kAtRegsLow, "softmax warpgroups would wait for registers forever");
-
-// two fp32 values in one 64-bit register and the packed instructions on them
-__device__ __forceinline__ uint64_t pack_b32x2(uint32_t lo, uint32_t hi) {
-  uint64_t v;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(lo), "r"(hi));
-  return v;
-}
-__device__ __forceinline__ uint64_t pack_f32x2(float lo, float hi) { return pack_b32x2(__float_as_uint(lo), __float_as_uint(hi)); }
-__device__ __forceinline__ void unpack_f32x2(uint64_t v, float& lo, float& hi) {
-  uint32_t a, b;
-  asm("mov.b64 {%0, %1}, %2;" : "=r"(a), "=r"(b) : "l"(v));
-  lo = __uint_as_float(a);
-  hi = __uint_as_float(b);
-}
-__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-// barrier among `count` threads (whole warps) that name the same id; ids 1..15 (0 is __syncthreads)
-__device__ __forceinline__ void named_barrier(int id, int count) {
-  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(count) : "memory");
-}
-
-// K-major operand, 128-byte swizzle (rows of 128 bytes, 8-row groups 1024 bytes apart)
-__device__ __forceinline__ uint64_t desc_kmajor(uint32_t addr) { return umma_desc_sw128(addr); }
-// MN-major operand, 128-byte swizzle: 64 contiguous elements of the M/N dimension per 128-byte row, one row
-// per k; 8-k groups `sbo` bytes apart, successive 64-element blocks of M/N `lbo` bytes apart.
-__device__ __forceinline__ uint64_t desc_mnmajor(uint32_t addr, uint32_t lbo, uint32_t sbo) {
-  uint64_t d = 0;
-  d |= static_cast<uint64_t>((addr >> 4) & 0x3fff);
-  d |= static_cast<uint64_t>((lbo >> 4) & 0x3fff) << 16;
-  d |= static_cast<uint64_t>((sbo >> 4) & 0x3fff) << 32;
-  d |= static_cast<uint64_t>(1) << 46;
-  d |= static_cast<uint64_t>(2) << 61;
-  return d;
-}
 
 template <int DH>
 struct AtSmem {

@@ -1,0 +1,147 @@
+// Device helpers of the 8-bit KV cache: the two code formats, the scale rule, and the arguments of its kernels.
+//
+// A page holds 64 tokens of every KV head; the codes of one (page, head) share one scale s = 2^e, e the smallest integer
+// in [kC8MinExp, kC8MaxExp] for which the largest magnitude of the rows is at most Q s (Q = 448 for e4m3, 127 for int8).
+// A power of two, because then (1) dividing by it is exact and a code is ONE rounding of the bf16 value; (2) raising the
+// scale of a page that grows re-rounds e4m3 codes only where they become subnormal; (3) every code times its scale is
+// exactly a bf16 number, and code and scale can be applied to different factors of a product without changing it.  It
+// costs at most one bit of an int8 code and nothing of an e4m3 code.
+// Rows that hold an infinity or a NaN, or whose magnitude does not fit 2^kC8MaxExp, make the scale NaN: every attention
+// that reads the page is NaN instead of quietly wrong.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+#include "kernels.h"
+
+namespace foe {
+
+constexpr int kC8MinExp = -32, kC8MaxExp = 64;
+constexpr int kC8E4M3 = 0, kC8Int8 = 1;
+
+// smallest exponent for a largest magnitude given as bf16 bits (sign cleared); INT_MAX when there is none.
+// amax = (1 + M / 2^7) 2^(E - 127); Q = 1.75 2^8 (e4m3) or 1.984375 2^6 (int8): e = E - 127 - 8 (6), one more if the
+// mantissa exceeds Q's.
+template <int FMT>
+__device__ __forceinline__ int c8_exponent(uint32_t amax_bits) {
+  constexpr int kQExp = FMT == kC8E4M3 ? 8 : 6;
+  constexpr uint32_t kQMan = FMT == kC8E4M3 ? 0x60 : 0x7e;        // of 7 bits
+  const int E = int(amax_bits >> 7);
+  if (E == 255) return 0x7fffffff;
+  int e = E - 127 - kQExp + ((amax_bits & 0x7f) > kQMan ? 1 : 0);
+  if (e > kC8MaxExp) return 0x7fffffff;
+  return max(e, kC8MinExp);
+}
+__device__ __forceinline__ float c8_pow2(int e) { return __int_as_float((e + 127) << 23); }   // -126 <= e <= 127
+// exponent of a stored scale (a power of two); only meaningful when the scale is finite
+__device__ __forceinline__ int c8_scale_exp(float s) { return int((__float_as_uint(s) >> 23) & 255) - 127; }
+__device__ __forceinline__ bool c8_is_nan(float s) { return (__float_as_uint(s) & 0x7fffffffu) > 0x7f800000u; }
+
+// four fp32 values (already divided by the scale, so |v| <= Q) -> four codes, element 0 in the lowest byte
+template <int FMT>
+__device__ __forceinline__ uint32_t c8_encode4(float a, float b, float c, float d) {
+  if constexpr (FMT == kC8E4M3) {
+    uint16_t lo, hi;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %2, %1;" : "=h"(lo) : "f"(a), "f"(b));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %2, %1;" : "=h"(hi) : "f"(c), "f"(d));
+    return uint32_t(lo) | (uint32_t(hi) << 16);
+  } else {
+    // adding 1.5 * 2^23 leaves the nearest integer (ties to even) in the low bits
+    constexpr float kMagic = 12582912.f;
+    const uint32_t x = __float_as_uint(a + kMagic), y = __float_as_uint(b + kMagic);
+    const uint32_t z = __float_as_uint(c + kMagic), w = __float_as_uint(d + kMagic);
+    return __byte_perm(__byte_perm(x, y, 0x0040), __byte_perm(z, w, 0x0040), 0x5410);
+  }
+}
+
+// two bytes of w (selected as a 16-bit half) -> two fp16 values, exactly (both formats fit fp16)
+__device__ __forceinline__ uint32_t c8_e4m3_pair(uint16_t h) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(h));
+  return r;
+}
+// natural order: lo = (byte 0, byte 1), hi = (byte 2, byte 3)
+template <int FMT>
+__device__ __forceinline__ void c8_decode_natural(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  if constexpr (FMT == kC8E4M3) {
+    lo = c8_e4m3_pair(uint16_t(w));
+    hi = c8_e4m3_pair(uint16_t(w >> 16));
+  } else {
+    // 0x6400 + u is the fp16 number 1024 + u for u < 1024; u = code + 128
+    const uint32_t x = w ^ 0x80808080u;
+    const __half2 off = __half2half2(__ushort_as_half(0x6480));           // 1152
+    const uint32_t a = __byte_perm(x, 0x64646464u, 0x4140), b = __byte_perm(x, 0x64646464u, 0x4342);
+    const __half2 ha = __hsub2(*reinterpret_cast<const __half2*>(&a), off), hb = __hsub2(*reinterpret_cast<const __half2*>(&b), off);
+    lo = *reinterpret_cast<const uint32_t*>(&ha);
+    hi = *reinterpret_cast<const uint32_t*>(&hb);
+  }
+}
+// split order: even = (byte 0, byte 2), odd = (byte 1, byte 3)
+template <int FMT>
+__device__ __forceinline__ void c8_decode_split(uint32_t w, uint32_t& even, uint32_t& odd) {
+  if constexpr (FMT == kC8E4M3) {
+    c8_decode_natural<FMT>(__byte_perm(w, 0, 0x3120), even, odd);
+  } else {
+    const uint32_t x = w ^ 0x80808080u;
+    const __half2 off = __half2half2(__ushort_as_half(0x6480));
+    const uint32_t a = __byte_perm(x, 0x64646464u, 0x4240), b = __byte_perm(x, 0x64646464u, 0x4341);
+    const __half2 ha = __hsub2(*reinterpret_cast<const __half2*>(&a), off), hb = __hsub2(*reinterpret_cast<const __half2*>(&b), off);
+    even = *reinterpret_cast<const uint32_t*>(&ha);
+    odd = *reinterpret_cast<const uint32_t*>(&hb);
+  }
+}
+// four codes -> four fp32 values
+template <int FMT>
+__device__ __forceinline__ void c8_decode4(uint32_t w, float (&v)[4]) {
+  uint32_t lo, hi;
+  c8_decode_natural<FMT>(w, lo, hi);
+  const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo)), b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+  v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+}
+// four codes at a scale 2^(-by) times larger: multiplied by `factor` = 2^(old - new) and rounded again
+template <int FMT>
+__device__ __forceinline__ uint32_t c8_rescale4(uint32_t w, float factor) {
+  float v[4];
+  c8_decode4<FMT>(w, v);
+  return c8_encode4<FMT>(v[0] * factor, v[1] * factor, v[2] * factor, v[3] * factor);
+}
+
+// ---- shared by the attention kernels
+__device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+// largest magnitude of 16 bytes of bf16, as bf16 bits
+__device__ __forceinline__ uint32_t c8_absmax(uint4 v) {
+  const uint32_t a = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+  return max(a & 0xffffu, a >> 16);
+}
+// exponent that brings a row with this largest magnitude to [2^7, 2^8): bf16 values within 2^31 of the largest are then
+// exact in fp16 or lose less than 2^-32 of it
+__device__ __forceinline__ int c8_query_exp(uint32_t amax_bits) {
+  const int E = int(amax_bits >> 7);
+  if (E == 255 || amax_bits == 0) return 0;
+  return max(E - 134, -60);
+}
+
+// sum of q_lens[0 .. b) by the whole block (every thread gets it); `red` = one int per warp of shared memory
+__device__ __forceinline__ int c8_block_prefix(const int* q_lens, int b, int* red) {
+  int s = 0;
+  for (int i = threadIdx.x; i < b; i += blockDim.x) s += max(q_lens[i], 0);
+  s = __reduce_add_sync(0xffffffffu, s);
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
+  __syncthreads();
+  int t = 0;
+  for (int w = 0; w < int(blockDim.x >> 5); ++w) t += red[w];
+  __syncthreads();
+  return t;
+}
+
+}  // namespace foe

@@ -1,0 +1,352 @@
+// C ABI of the 8-bit KV cache (see include/foe_cache.h): argument checks, workspace, tensor maps, launches.
+#include <math.h>
+#include <string.h>
+
+#include <new>
+
+#include "cache8.cuh"
+#include "cache8_handle.h"
+#include "tensor_map.h"
+
+using namespace foe;
+
+namespace {
+
+bool off(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+
+// One allocation for the whole workspace: the first pass over the buffers adds up their sizes, the second hands them out.
+struct Arena {
+  uint8_t* base = nullptr;
+  size_t used = 0;
+  template <typename T>
+  void take(T** p, size_t count) {
+    if (base) *p = reinterpret_cast<T*>(base + used);
+    used += (count * sizeof(T) + 255) / 256 * 256;
+  }
+};
+
+void lay_out(foe_cache* h, Arena* m) {
+  const foe_cache_config& c = h->cfg;
+  const size_t dhp = c.head_dim > 64 ? 128 : 64;
+  const size_t d_rows = cache8_decode_part_rows(h->n_sms), c_rows = cache8_chunk_part_rows(h->n_sms);
+  const size_t rows = d_rows > c_rows ? d_rows : c_rows;
+  m->take(&h->status, 1);                                  // zeroed at creation, with split_done behind it
+  m->take(&h->split_done, h->split_done_count);
+  m->take(&h->part_ml, rows * 2);
+  m->take(&h->part_o, rows * dhp);
+  if (c.track_weights) {
+    m->take(&h->lse, size_t(h->rows_max) * c.n_q_heads);
+    m->take(&h->logits, size_t(c.max_seqs) * c.n_q_heads * size_t(h->logits_stride));
+  }
+  if (c.for_layers) {
+    const size_t stage = (size_t(h->rows_max) + 63) / 64 * 64 * c.n_kv_heads * c.head_dim;
+    m->take(&h->k_stage, stage);
+    m->take(&h->v_stage, stage);
+    m->take(&h->tok_pos, h->rows_max);
+    m->take(&h->tok_slot, h->rows_max);
+  }
+}
+
+// codes of all pages as rows of head_dim bytes; a box is one page of one head, rows padded with zeros to 128 bytes
+bool make_code_map(CUtensorMap* m, const void* base, uint64_t rows, uint64_t dh) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (!fn) return false;
+  const cuuint64_t gdim[2] = {dh, rows};
+  const cuuint64_t gstride[1] = {dh};
+  const cuuint32_t box[2] = {128, 64};
+  const cuuint32_t estr[2] = {1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+foe_status check_config(const foe_cache_config* c) {
+  if (c->n_q_heads <= 0 || c->n_kv_heads <= 0 || c->n_q_heads % c->n_kv_heads || c->n_q_heads / c->n_kv_heads > 16) return FOE_ERR_CONFIG;
+  if (c->n_kv_heads > 65535) return FOE_ERR_CONFIG;
+  if (c->head_dim != 64 && c->head_dim != 96 && c->head_dim != 128) return FOE_ERR_CONFIG;
+  if (c->page_size != 64 || (c->format != FOE_CACHE_E4M3 && c->format != FOE_CACHE_INT8)) return FOE_ERR_CONFIG;
+  if (c->max_tokens <= 0 || c->max_seqs <= 0 || c->max_seqs > 65535 || c->max_context <= 0) return FOE_ERR_CONFIG;
+  return FOE_OK;
+}
+
+bool right_device(const foe_cache* h) {
+  int dev = -1;
+  return cudaGetDevice(&dev) == cudaSuccess && dev == h->device;
+}
+
+foe_status launched() { return cudaGetLastError() == cudaSuccess ? FOE_OK : FOE_ERR_CUDA; }
+
+}  // namespace
+
+namespace foe {
+
+foe_status cache8_check(const foe_cache* h, const foe_cache_view* v, bool need_q, int* rows) {
+  *rows = 0;
+  if (v->n_seqs == 0) return FOE_OK;             // (arrays of no sequences may have no address)
+  if (!v->k_pages || !v->v_pages || !v->k_scales || !v->v_scales || !v->block_table || !v->context_lens) return FOE_ERR_NULL;
+  if (off(v->k_pages, 16) || off(v->v_pages, 16) || off(v->k_scales, 4) || off(v->v_scales, 4) || off(v->block_table, 4) ||
+      off(v->context_lens, 4) || off(v->q_lens, 4) || off(v->positions, 4))
+    return FOE_ERR_SHAPE;
+  if (v->n_seqs < 0 || v->n_seqs > h->cfg.max_seqs || v->max_pages_per_seq <= 0 || v->num_pages <= 0) return FOE_ERR_SHAPE;
+  // rows of codes are numbered with 32-bit integers (2^31 rows of 128 codes are 256 GiB)
+  if ((long long)v->num_pages * h->cfg.n_kv_heads * 64 >= (1LL << 31)) return FOE_ERR_SHAPE;
+  *rows = v->n_seqs;
+  if (need_q && v->q_lens) {
+    if (v->n_tokens < 0 || v->n_tokens > h->cfg.max_tokens) return FOE_ERR_SHAPE;
+    if (v->n_tokens > 0 && (v->max_q_len <= 0 || v->max_q_len > v->n_tokens)) return FOE_ERR_SHAPE;
+    if ((long long)v->n_seqs * ((v->max_q_len + 126) / 64) >= (1LL << 31)) return FOE_ERR_SHAPE;
+    if ((long long)v->n_seqs * ((v->max_q_len + 127) / 128) * h->cfg.n_q_heads >= (1LL << 31)) return FOE_ERR_SHAPE;
+    *rows = v->n_tokens;
+  }
+  if (!v->q_lens) {
+    const Cache8Args c = cache8_args(h, v, nullptr);
+    // the decode kernel numbers the pages of all (sequence, KV head) pairs with 32-bit integers
+    if ((long long)v->n_seqs * h->cfg.n_kv_heads * c.max_kv_pages >= (1LL << 30)) return FOE_ERR_SHAPE;
+  }
+  return FOE_OK;
+}
+
+foe_status cache8_check_weights(const foe_cache* h, const foe_cache_view* v, const float* in, const float* out, long long stride, int window) {
+  if ((!in && !out) || v->n_seqs == 0) return FOE_OK;
+  if (!in || !out) return FOE_ERR_NULL;
+  if (!h->cfg.track_weights) return FOE_ERR_UNSUPPORTED;
+  if (window < 0 || off(in, 4) || off(out, 4)) return FOE_ERR_SHAPE;
+  return stride >= cache8_args(h, v, nullptr).max_len ? FOE_OK : FOE_ERR_SHAPE;
+}
+
+Cache8Args cache8_args(const foe_cache* h, const foe_cache_view* v, int* status) {
+  Cache8Args c;
+  c.k_pages = static_cast<uint8_t*>(v->k_pages); c.v_pages = static_cast<uint8_t*>(v->v_pages);
+  c.k_scales = v->k_scales; c.v_scales = v->v_scales;
+  c.block_table = v->block_table; c.context_lens = v->context_lens; c.q_lens = v->q_lens;
+  c.n_seqs = v->n_seqs; c.max_pages_per_seq = v->max_pages_per_seq; c.num_pages = v->num_pages;
+  c.n_tokens = v->q_lens ? v->n_tokens : v->n_seqs; c.max_q_len = v->q_lens ? v->max_q_len : 1;
+  c.n_q = h->cfg.n_q_heads; c.n_kv = h->cfg.n_kv_heads; c.dh = h->cfg.head_dim;
+  const long long table = (long long)v->max_pages_per_seq * 64;
+  c.max_len = int(table < h->cfg.max_context ? table : h->cfg.max_context);
+  c.max_kv_pages = (c.max_len + 63) / 64;
+  c.status = status;
+  return c;
+}
+
+int cache8_attend(foe_cache* h, const foe_cache_view* v, const void* q, long long q_stride, int q_head_stride, void* out,
+                  long long out_stride, const float* w_in, float* w_out, long long w_stride, int window, int* status, cudaStream_t st) {
+  Cache8AttendArgs a;
+  memset(&a, 0, sizeof(a));
+  a.c = cache8_args(h, v, status);
+  a.q = static_cast<const __nv_bfloat16*>(q); a.q_stride = q_stride; a.q_head_stride = q_head_stride;
+  a.out = static_cast<__nv_bfloat16*>(out); a.out_stride = out_stride;
+  a.scale_log2 = float(1.4426950408889634 / sqrt(double(a.c.dh)));
+  a.part_o = h->part_o; a.part_ml = h->part_ml; a.split_done = h->split_done;
+  if (w_out) { a.lse = h->lse; a.logits = h->logits; a.logits_stride = h->logits_stride; }
+  const uint64_t rows = uint64_t(a.c.num_pages) * a.c.n_kv * 64;
+  CUtensorMap tmK, tmV;
+  if (!make_code_map(&tmK, v->k_pages, rows, a.c.dh) || !make_code_map(&tmV, v->v_pages, rows, a.c.dh)) return -1;
+  int n = 1;
+  if (!v->q_lens) launch_cache8_decode(h->cfg.format, tmK, tmV, a, h->n_sms, st);
+  else n = launch_cache8_chunk(h->cfg.format, tmK, tmV, a, h->n_sms, st);
+  if (w_out) {
+    Cache8WeightsArgs w;
+    w.a = a; w.weights_in = w_in; w.weights_out = w_out; w.weights_stride = w_stride; w.window = window;
+    launch_cache8_weights(h->cfg.format, w, st);
+    n += 1;
+  }
+  return n;
+}
+
+void cache8_append_staged(foe_cache* h, const foe_cache_view* v, int* status, cudaStream_t st) {
+  Cache8AppendArgs a;
+  a.c = cache8_args(h, v, status);
+  a.k = h->k_stage; a.v = h->v_stage;
+  a.k_lay.row = a.v_lay.row = a.c.dh;
+  a.k_lay.head = a.v_lay.head = 64 * a.c.dh;
+  a.k_lay.tile = a.v_lay.tile = (long long)a.c.n_kv * 64 * a.c.dh;
+  launch_cache8_append(h->cfg.format, a, st);
+}
+
+// One block per sequence (decode: one block for all of them).
+__global__ void cache8_token_map_kernel(const int* q_lens, const int* positions, int n_seqs, int n_tokens, int max_context,
+                                        int* tok_pos, int* tok_slot, int* status) {
+  pdl_wait();
+  pdl_launch_dependents();
+  __shared__ int red[8];
+  auto put = [&](int t, int pos) {
+    const bool bad = pos < 0 || pos >= max_context;
+    if (bad) atomicExch(status, kStatusBounds);
+    tok_pos[t] = min(max(pos, 0), max_context - 1);
+    tok_slot[t] = t;
+  };
+  if (!q_lens) {
+    for (int b = blockIdx.x * blockDim.x + threadIdx.x; b < n_seqs; b += gridDim.x * blockDim.x) put(b, positions[b]);
+    return;
+  }
+  const int b = blockIdx.x;
+  const int start = c8_block_prefix(q_lens, b, red);
+  const int q_len = max(q_lens[b], 0), pos = positions[b];
+  for (int i = threadIdx.x; i < q_len && start + i < n_tokens; i += blockDim.x) put(start + i, pos + i);
+  // tokens that no sequence claims (lengths that do not add up) get a position and their own slot all the same
+  if (b == n_seqs - 1) {
+    if (threadIdx.x == 0 && start + q_len != n_tokens) atomicExch(status, kStatusBounds);
+    for (int t = start + q_len + threadIdx.x; t < n_tokens; t += blockDim.x) { tok_pos[t] = 0; tok_slot[t] = t; }
+  }
+}
+
+void launch_cache8_token_map(const int* q_lens, const int* positions, int n_seqs, int n_tokens, int max_context, int* tok_pos,
+                             int* tok_slot, int* status, cudaStream_t st) {
+  const int grid = q_lens ? n_seqs : (n_seqs + 255) / 256;
+  launch_pdl(cache8_token_map_kernel, dim3(grid), dim3(256), 0, st, q_lens, positions, n_seqs, n_tokens, max_context, tok_pos, tok_slot, status);
+}
+
+}  // namespace foe
+
+extern "C" {
+
+foe_status foe_cache_destroy(foe_cache* h) {
+  if (!h) return FOE_OK;
+  cudaFree(h->memory);
+  delete h;
+  return FOE_OK;
+}
+
+foe_status foe_cache_create(const foe_cache_config* cfg, foe_cache** out) {
+  if (!cfg || !out) return FOE_ERR_NULL;
+  *out = nullptr;
+  const foe_status v = check_config(cfg);
+  if (v != FOE_OK) return v;
+  int dev = 0, n_dev = 0;
+  if (cudaGetDeviceCount(&n_dev) != cudaSuccess || n_dev == 0) { cudaGetLastError(); return FOE_ERR_CUDA; }
+  if (cudaGetDevice(&dev) != cudaSuccess) return FOE_ERR_CUDA;
+  int major = 0, sms = 0;
+  if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return FOE_ERR_CUDA;
+  if (major != 10) return FOE_ERR_UNSUPPORTED;            // tcgen05 kernels: sm_100 only
+  if (cache8_decode_configure() != cudaSuccess || cache8_chunk_configure() != cudaSuccess) { cudaGetLastError(); return FOE_ERR_CUDA; }
+  foe_cache* h = new (std::nothrow) foe_cache();
+  if (!h) return FOE_ERR_OOM;
+  h->cfg = *cfg;
+  h->device = dev;
+  h->n_sms = sms;
+  h->rows_max = cfg->max_tokens > cfg->max_seqs ? cfg->max_tokens : cfg->max_seqs;
+  h->split_done_count = size_t(cfg->max_seqs) * cfg->n_kv_heads;
+  h->logits_stride = ((long long)cfg->max_context + 63) / 64 * 64;
+  Arena sizes;
+  lay_out(h, &sizes);
+  Arena mem;
+  if (cudaMalloc(reinterpret_cast<void**>(&mem.base), sizes.used) != cudaSuccess) {
+    cudaGetLastError();
+    delete h;
+    return FOE_ERR_OOM;
+  }
+  h->memory = mem.base;
+  lay_out(h, &mem);
+  const size_t zeroed = reinterpret_cast<uint8_t*>(h->part_ml) - mem.base;
+  if (cudaMemset(mem.base, 0, zeroed) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
+    cudaGetLastError();
+    foe_cache_destroy(h);
+    return FOE_ERR_CUDA;
+  }
+  *out = h;
+  return FOE_OK;
+}
+
+foe_status foe_cache_append(foe_cache* h, const void* k, long long k_stride, const void* v, long long v_stride,
+                            const foe_cache_view* view, void* stream) {
+  if (!h || !view) return FOE_ERR_NULL;
+  int rows = 0;
+  const foe_status s = cache8_check(h, view, true, &rows);
+  if (s != FOE_OK) return s;
+  if (rows == 0) return FOE_OK;
+  if (!k || !v) return FOE_ERR_NULL;
+  const long long width = (long long)h->cfg.n_kv_heads * h->cfg.head_dim;
+  if (off(k, 16) || off(v, 16) || k_stride % 8 || v_stride % 8 || k_stride < width || v_stride < width) return FOE_ERR_SHAPE;
+  if (!right_device(h)) return FOE_ERR_UNSUPPORTED;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  h->last_stream = st;
+  g_overlap_launches = true;
+  Cache8AppendArgs a;
+  a.c = cache8_args(h, view, h->status);
+  a.k = static_cast<const __nv_bfloat16*>(k); a.v = static_cast<const __nv_bfloat16*>(v);
+  a.k_lay.row = k_stride; a.v_lay.row = v_stride;
+  a.k_lay.head = a.v_lay.head = h->cfg.head_dim;
+  a.k_lay.tile = 64 * k_stride; a.v_lay.tile = 64 * v_stride;
+  launch_cache8_append(h->cfg.format, a, st);
+  return launched();
+}
+
+foe_status foe_cache_attend(foe_cache* h, const void* q, long long q_stride, const foe_cache_view* view, void* out,
+                            long long out_stride, const float* weights_in, float* weights_out, long long weights_stride,
+                            int window, void* stream) {
+  if (!h || !view) return FOE_ERR_NULL;
+  int rows = 0;
+  const foe_status s = cache8_check(h, view, true, &rows);
+  if (s != FOE_OK) return s;
+  const foe_status w = cache8_check_weights(h, view, weights_in, weights_out, weights_stride, window);
+  if (w != FOE_OK) return w;
+  if (rows == 0 && !(weights_out && view->n_seqs > 0)) return FOE_OK;
+  if (rows > 0 && (!q || !out)) return FOE_ERR_NULL;
+  const long long width = (long long)h->cfg.n_q_heads * h->cfg.head_dim;
+  if (off(q, 16) || off(out, 16) || q_stride % 8 || out_stride % 8 || q_stride < width || out_stride < width) return FOE_ERR_SHAPE;
+  if (q && q == out) return FOE_ERR_UNSUPPORTED;
+  if (!right_device(h)) return FOE_ERR_UNSUPPORTED;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  h->last_stream = st;
+  g_overlap_launches = true;
+  if (cache8_attend(h, view, q, q_stride, h->cfg.head_dim, out, out_stride, weights_in, weights_out, weights_stride, window, h->status, st) < 0)
+    return FOE_ERR_CUDA;
+  return launched();
+}
+
+foe_status foe_cache_evict(foe_cache* h, const foe_cache_view* view, const float* weights, long long weights_stride,
+                           const int* to_table, int to_pages_per_seq, int budget, int sink, int recent, int* new_lens,
+                           int* kept, float* weights_out, long long weights_out_stride, void* stream) {
+  if (!h || !view) return FOE_ERR_NULL;
+  int rows = 0;
+  const foe_status s = cache8_check(h, view, false, &rows);
+  if (s != FOE_OK) return s;
+  if (budget < 1 || sink < 0 || recent < 0 || sink > budget || recent > budget - sink || to_pages_per_seq <= 0 ||
+      (long long)to_pages_per_seq * 64 < budget)
+    return FOE_ERR_SHAPE;
+  if (view->n_seqs == 0) return FOE_OK;
+  if (!weights || !to_table || !new_lens || !kept) return FOE_ERR_NULL;
+  if (off(weights, 4) || off(to_table, 4) || off(new_lens, 4) || off(kept, 4) || off(weights_out, 4)) return FOE_ERR_SHAPE;
+  Cache8EvictArgs a;
+  a.c = cache8_args(h, view, h->status);
+  if (weights_stride < a.c.max_len || (weights_out && weights_out_stride < budget)) return FOE_ERR_SHAPE;
+  if ((long long)view->n_seqs * ((budget + 63) / 64) >= (1LL << 31)) return FOE_ERR_SHAPE;
+  if (weights_out == weights) return FOE_ERR_UNSUPPORTED;
+  if (!right_device(h)) return FOE_ERR_UNSUPPORTED;
+  a.weights = weights; a.weights_stride = weights_stride; a.to_table = to_table; a.to_pages_per_seq = to_pages_per_seq;
+  a.budget = budget; a.sink = sink; a.recent = recent; a.new_lens = new_lens; a.kept = kept;
+  a.weights_out = weights_out; a.weights_out_stride = weights_out_stride;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  h->last_stream = st;
+  g_overlap_launches = true;
+  launch_cache8_evict(h->cfg.format, a, st);
+  return launched();
+}
+
+foe_status foe_cache_check(const foe_cache_config* cfg, const foe_cache_view* view) {
+  if (!cfg || !view) return FOE_ERR_NULL;
+  const foe_status v = check_config(cfg);
+  if (v != FOE_OK) return v;
+  int rows = 0;
+  foe_cache h = {};
+  h.cfg = *cfg;
+  return cache8_check(&h, view, true, &rows);
+}
+
+foe_status foe_cache_poll_status(foe_cache* h, int* device_status) {
+  if (!h || !device_status) return FOE_ERR_NULL;
+  if (cudaStreamSynchronize(h->last_stream) != cudaSuccess) { cudaGetLastError(); return FOE_ERR_CUDA; }
+  int v = 0;
+  if (cudaMemcpy(&v, h->status, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) return FOE_ERR_CUDA;
+  *device_status = v;
+  if (v != 0) {
+    cudaMemset(h->status, 0, sizeof(int));
+    // the counters re-arm themselves; after a reported failure make sure of it
+    cudaMemset(h->split_done, 0, h->split_done_count * sizeof(int));
+  }
+  return FOE_OK;
+}
+
+}  // extern "C"

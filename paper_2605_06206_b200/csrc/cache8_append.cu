@@ -1,0 +1,186 @@
+// Writing K and V rows into the 8-bit cache (see cache8.cuh for the formats and the scale rule).
+//
+// The rows of one (page, KV head) share a scale, so that unit is what one block or warp works on: it holds its rows in
+// registers, takes their largest magnitude (an integer maximum over the bf16 bits), and encodes them.  Rows that the
+// page holds already are only touched when its scale grows; they are then rounded again at the new one.
+// Bound: memory (2 bytes read and 1 written per element), launch latency for single tokens.
+#include "cache8.cuh"
+#include "cache8.h"
+
+namespace foe {
+
+__device__ __forceinline__ uint32_t absmax_bf16x2(uint32_t a, uint32_t b) { return __vmaxu2(a & 0x7fff7fffu, b & 0x7fff7fffu); }
+
+// ------------------------------------------------------------------------------------------- one token a sequence
+// One warp per (sequence, KV head, K or V).
+constexpr int kApWarps = 4;
+template <int FMT>
+__global__ void __launch_bounds__(kApWarps * 32)
+cache8_append_token_kernel(const Cache8AppendArgs a) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const Cache8Args& c = a.c;
+  const int lane = threadIdx.x & 31;
+  const long long item = (long long)blockIdx.x * kApWarps + (threadIdx.x >> 5);
+  if (item >= 2LL * c.n_seqs * c.n_kv) return;
+  const int kvh = int(item % c.n_kv);
+  const int b = int((item / c.n_kv) % c.n_seqs);
+  const bool is_v = item >= (long long)c.n_seqs * c.n_kv;
+  const int pos = c.context_lens[b];
+  if (pos < 0 || pos >= c.max_len) {
+    if (lane == 0) atomicExch(c.status, kStatusBounds);
+    return;
+  }
+  const int page = c.block_table[size_t(b) * c.max_pages_per_seq + (pos >> 6)];
+  if (page < 0 || page >= c.num_pages) {
+    if (lane == 0) atomicExch(c.status, kStatusBounds);
+    return;
+  }
+  const size_t ph = size_t(page) * c.n_kv + kvh;
+  const int row = pos & 63;
+  float* scale_p = (is_v ? c.v_scales : c.k_scales) + ph;
+  uint32_t* codes = reinterpret_cast<uint32_t*>((is_v ? c.v_pages : c.k_pages) + ph * 64 * c.dh);
+  const Cache8Rows& lay = is_v ? a.v_lay : a.k_lay;
+  const __nv_bfloat16* src = (is_v ? a.v : a.k) + (b >> 6) * lay.tile + (b & 63) * lay.row + kvh * lay.head;
+  const bool have = lane * 4 < c.dh;                       // four elements a lane (head_dim is 64, 96 or 128)
+  uint2 x = make_uint2(0, 0);
+  if (have) x = *reinterpret_cast<const uint2*>(src + lane * 4);
+  const float held = row > 0 ? *scale_p : 1.f;
+  const uint32_t m2 = absmax_bf16x2(x.x, x.y);
+  const uint32_t amax = __reduce_max_sync(0xffffffffu, max(m2 & 0xffffu, m2 >> 16));
+  int e = c8_exponent<FMT>(amax);
+  const bool nan = e == 0x7fffffff || c8_is_nan(held);
+  float scale = __int_as_float(0x7fc00000);
+  uint32_t code = 0;
+  if (!nan) {
+    const int e_held = c8_scale_exp(held);
+    if (row > 0 && e_held > e) e = e_held;
+    if (row > 0 && e > e_held) {                           // the page's scale grows: its rows are rounded again
+      const float f = c8_pow2(e_held - e);
+      for (int i = lane; i < row * (c.dh >> 2); i += 32) codes[i] = c8_rescale4<FMT>(codes[i], f);
+    }
+    scale = c8_pow2(e);
+    const float inv = c8_pow2(-e);
+    code = c8_encode4<FMT>(bf16_lo(x.x) * inv, bf16_hi(x.x) * inv, bf16_lo(x.y) * inv, bf16_hi(x.y) * inv);
+  }
+  if (have) codes[row * (c.dh >> 2) + lane] = code;
+  if (lane == 0) *scale_p = scale;
+}
+
+// ------------------------------------------------------------------------------------------- chunks
+// One block of 256 threads per (sequence, page the chunk touches, KV head, K or V); a thread holds 8 elements of DH / 32
+// rows (64 rows x DH elements over 256 threads).
+constexpr int kApThreads = 256;
+template <int FMT, int DH>
+__global__ void __launch_bounds__(kApThreads)
+cache8_append_chunk_kernel(const Cache8AppendArgs a, const int blocks_per_seq) {
+  pdl_wait();
+  pdl_launch_dependents();
+  __shared__ int red[kApThreads / 32];
+  __shared__ uint32_t redm[kApThreads / 32];
+  const Cache8Args& c = a.c;
+  constexpr int CH = DH / 8;                               // 8-element pieces of a row
+  constexpr int PER = 64 * CH / kApThreads;                // pieces a thread holds
+  const int b = blockIdx.x / blocks_per_seq, slot = blockIdx.x - b * blocks_per_seq;
+  const int kvh = blockIdx.y;
+  const bool is_v = blockIdx.z != 0;
+  const int ctx = c.context_lens[b], q_len = c.q_lens[b];
+  if (q_len <= 0) {
+    if (q_len < 0 && threadIdx.x == 0) atomicExch(c.status, kStatusBounds);
+    return;
+  }
+  const bool bad = ctx < 0 || q_len > c.max_q_len || (long long)ctx + q_len > c.max_len;
+  const int blk = bad ? 0 : (ctx >> 6) + slot;
+  if (!bad && blk * 64 >= ctx + q_len) return;
+  const int tok0 = c8_block_prefix(c.q_lens, b, red);
+  if (bad || tok0 + q_len > c.n_tokens) {                  // the call's lengths disagree with what the host was told
+    if (threadIdx.x == 0) atomicExch(c.status, kStatusBounds);
+    return;
+  }
+  const int page = c.block_table[size_t(b) * c.max_pages_per_seq + blk];
+  if (page < 0 || page >= c.num_pages) {
+    if (threadIdx.x == 0) atomicExch(c.status, kStatusBounds);
+    return;
+  }
+  const int first = max(ctx - blk * 64, 0);                // rows the page holds already
+  const int last = min(ctx + q_len - blk * 64, 64);        // rows [first, last) are new
+  const size_t ph = size_t(page) * c.n_kv + kvh;
+  float* scale_p = (is_v ? c.v_scales : c.k_scales) + ph;
+  uint2* codes = reinterpret_cast<uint2*>((is_v ? c.v_pages : c.k_pages) + ph * 64 * DH);
+  const Cache8Rows& lay = is_v ? a.v_lay : a.k_lay;
+  const __nv_bfloat16* src = (is_v ? a.v : a.k) + kvh * lay.head;
+  const int tok_row0 = tok0 + blk * 64 - ctx;              // token of the page's row 0 (rows before `first` are older)
+  uint4 x[PER];
+  uint32_t m2 = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int p = i * kApThreads + threadIdx.x, row = p / CH, ch = p - row * CH;
+    x[i] = make_uint4(0, 0, 0, 0);
+    if (row >= first && row < last) {
+      const int t = tok_row0 + row;
+      x[i] = *reinterpret_cast<const uint4*>(src + (t >> 6) * lay.tile + (t & 63) * lay.row + ch * 8);
+    }
+    m2 = __vmaxu2(m2, __vmaxu2(absmax_bf16x2(x[i].x, x[i].y), absmax_bf16x2(x[i].z, x[i].w)));
+  }
+  const float held = first > 0 ? *scale_p : 1.f;
+  const uint32_t wmax = __reduce_max_sync(0xffffffffu, max(m2 & 0xffffu, m2 >> 16));
+  if ((threadIdx.x & 31) == 0) redm[threadIdx.x >> 5] = wmax;
+  __syncthreads();                                         // (also: `held` has been read by every thread)
+  uint32_t amax = 0;
+#pragma unroll
+  for (int w = 0; w < kApThreads / 32; ++w) amax = max(amax, redm[w]);
+  int e = c8_exponent<FMT>(amax);
+  const bool nan = e == 0x7fffffff || c8_is_nan(held);
+  float f = 1.f, inv = 0.f, scale = __int_as_float(0x7fc00000);
+  if (!nan) {
+    const int e_held = c8_scale_exp(held);
+    if (first > 0) {
+      e = max(e, e_held);
+      f = c8_pow2(e_held - e);
+    }
+    inv = c8_pow2(-e);
+    scale = c8_pow2(e);
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int p = i * kApThreads + threadIdx.x, row = p / CH;
+    uint2 v;
+    if (row < first) {
+      if (f == 1.f) continue;                              // the rows the page holds keep their codes
+      v = codes[p];
+      v = make_uint2(c8_rescale4<FMT>(v.x, f), c8_rescale4<FMT>(v.y, f));
+    } else if (row < last) {
+      v = make_uint2(0, 0);
+      if (!nan)
+        v = make_uint2(c8_encode4<FMT>(bf16_lo(x[i].x) * inv, bf16_hi(x[i].x) * inv, bf16_lo(x[i].y) * inv, bf16_hi(x[i].y) * inv),
+                       c8_encode4<FMT>(bf16_lo(x[i].z) * inv, bf16_hi(x[i].z) * inv, bf16_lo(x[i].w) * inv, bf16_hi(x[i].w) * inv));
+    } else {
+      continue;                                            // rows behind the last token stay as they were
+    }
+    codes[p] = v;
+  }
+  if (threadIdx.x == 0) *scale_p = scale;
+}
+
+template <int FMT>
+static void launch_append_t(const Cache8AppendArgs& a, cudaStream_t st) {
+  const Cache8Args& c = a.c;
+  if (!c.q_lens) {
+    const long long items = 2LL * c.n_seqs * c.n_kv;
+    launch_pdl(cache8_append_token_kernel<FMT>, dim3(unsigned((items + kApWarps - 1) / kApWarps)), dim3(kApWarps * 32), 0, st, a);
+    return;
+  }
+  const int per_seq = (c.max_q_len + 126) / 64;            // pages a chunk of that length can touch
+  const dim3 grid(unsigned(c.n_seqs) * per_seq, c.n_kv, 2);
+  if (c.dh == 64) launch_pdl(cache8_append_chunk_kernel<FMT, 64>, grid, dim3(kApThreads), 0, st, a, per_seq);
+  else if (c.dh == 96) launch_pdl(cache8_append_chunk_kernel<FMT, 96>, grid, dim3(kApThreads), 0, st, a, per_seq);
+  else launch_pdl(cache8_append_chunk_kernel<FMT, 128>, grid, dim3(kApThreads), 0, st, a, per_seq);
+}
+
+void launch_cache8_append(int fmt, const Cache8AppendArgs& a, cudaStream_t st) {
+  if (a.c.n_seqs <= 0 || a.c.n_tokens <= 0) return;
+  if (fmt == kC8E4M3) launch_append_t<kC8E4M3>(a, st);
+  else launch_append_t<kC8Int8>(a, st);
+}
+
+}  // namespace foe

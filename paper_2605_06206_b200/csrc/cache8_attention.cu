@@ -1,0 +1,503 @@
+// Attention of single new tokens over the 8-bit cache, and the accumulation of attention weights.
+//
+// Decode reads every code of the cache once: 1 byte per K and V element, so the kernel has half the time per element of
+// a bf16 one and its arithmetic has to be lean.
+//   * Codes become fp16 in registers (exactly; both formats fit) and are never scaled: the K scale multiplies the
+//     scores, the V scale enters the exponent, t = s + log2(scale_v), so that P' = 2^(t - m) already carries it.  The
+//     row sum takes 2^-log2(scale_v) back out.
+//   * The keys are the M side of both products, the g query heads of a KV head the N side (8 columns for g <= 8):
+//     S^T = K q^T and O^T = V^T P^T, half the mma.sync instructions of the orientation with the heads as M, whose 16
+//     rows a group of 2 to 8 heads leaves mostly empty.  P^T changes layout in registers with movmatrix.
+//   * The contraction order over head_dim is free, so a lane's K fragment is 16 consecutive codes of a row (one
+//     128-bit load for four k-steps), and the query fragments are loaded from global memory in the same order.  The key
+//     order inside a group of 16 is free too and chosen so that those loads touch every bank once.
+//   * V fragments come from ldmatrix.trans on pairs of codes: a register holds two keys of dims 2i, 2i + 1, which split
+//     into the even and the odd dims of a 16-dim tile.
+//   * The running maximum is only moved when a score exceeds it by 2^8 (one vote per 16 keys), so that neither the
+//     maximum's shuffles nor the rescaling of the accumulators is in the common path.  P' is kept 2^6 above its natural
+//     scale: fp16 then loses a probability only below 2^-30 of the largest.
+// CTAs are persistent, two per SM, a producer warp streaming pages (one TMA box each for K and V) through a ring; the
+// consumer warps are two groups of four that take alternate pages, a warp 16 keys of its page.  The call's pages are
+// divided evenly (decode_walk.cuh).  A CTA's range can cut at most two pairs (its first and its last), so partial
+// results live in two slots per CTA, and the last CTA of a pair to finish merges them in CTA order.
+#include <math.h>
+
+#include "cache8.cuh"
+#include "cache8.h"
+#include "decode_walk.cuh"
+
+namespace foe {
+
+constexpr int kD8Stages = 6;
+constexpr int kD8MinTiles = 2;                   // fewest pages per CTA
+constexpr float kD8Shift = 6.f;                  // P' = 2^(t - m + shift)
+constexpr float kD8Lazy = 8.f;                   // the reference maximum moves when a score exceeds it by more than this
+
+template <int NT> struct D8Cfg {                 // NT: tiles of 8 heads
+  static constexpr int kWarps = NT == 1 ? 8 : 4; // consumers (16 heads: fewer warps with twice the registers)
+  static constexpr int kGroups = kWarps / 4;     // groups of four warps that take alternate pages
+  static constexpr int kThreads = (kWarps + 1) * 32;
+  // A stage belongs to one group for good, so that the group sees every phase of the stage's barrier: a parity wait
+  // cannot tell a phase from the one before the last.
+  static_assert(kD8Stages % kGroups == 0, "stages are divided among the groups");
+};
+
+template <int DH, int NT>
+struct D8Smem {
+  static constexpr int kTile = 64 * 128;         // codes of a page of one head, rows padded to 128 bytes by the TMA box
+  static constexpr int kRing = kD8Stages * 2 * kTile;
+  static constexpr int kPitch = DH + 8;
+  static constexpr int kRows = 8 * NT;
+  static constexpr int kMoOff = kRing;
+  static constexpr int kMmOff = kMoOff + kRows * kPitch * 4;                     // [warps][kRows] maxima, then sums
+  static constexpr int kScaleOff = kMmOff + 2 * D8Cfg<NT>::kWarps * kRows * 4;   // per stage: K scale, log2 V scale, 1 / V scale
+  static constexpr int kBarOff = kScaleOff + kD8Stages * 16;
+  static constexpr int kMiscOff = kBarOff + 2 * kD8Stages * 8;
+  static constexpr size_t kBytes = size_t(kMiscOff) + 16 + 1024;
+};
+
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+  return v;
+}
+template <int THREADS>
+__device__ __forceinline__ void d8_bar() { asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory"); }
+
+template <int FMT, int DH, int NT>
+__global__ void __launch_bounds__(D8Cfg<NT>::kThreads, 2)
+cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const Cache8AttendArgs a) {
+  using SM = D8Smem<DH, NT>;
+  using CF = D8Cfg<NT>;
+  constexpr int NC = DH / 16;                                      // 16-code chunks of a row
+  constexpr int CT = CF::kWarps * 32;                              // consumer threads
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  float* mo = reinterpret_cast<float*>(smem + SM::kMoOff);
+  float* mm = reinterpret_cast<float*>(smem + SM::kMmOff);
+  float* ml = mm + CF::kWarps * SM::kRows;
+  float4* scales = reinterpret_cast<float4*>(smem + SM::kScaleOff);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + SM::kBarOff);
+  uint64_t* empty = full + kD8Stages;
+  int* ticket_s = reinterpret_cast<int*>(smem + SM::kMiscOff);
+  const Cache8Args& c = a.c;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kD8Stages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 4); }
+    mbar_fence_init();
+  }
+  __syncthreads();
+  pdl_wait();
+  pdl_launch_dependents();
+
+  DcWalk w;
+  if (!dc_begin(c, kD8MinTiles, w)) return;                        // (the same in every warp)
+
+  if (warp == CF::kWarps) {
+    // ------------------------------------------------------------------ producer
+    bool ok = true;
+    int it = 0;
+    while (ok && w.t < w.t_end) {
+      const int len = dc_segment_len(w);
+      for (int j0 = 0; j0 < len && ok; j0 += 32) {
+        const int n = min(32, len - j0);
+        int row0 = 0;
+        float sk = 0.f, sv = 1.f;
+        if (lane < n) {
+          const int lp = w.page + j0 + lane;
+          int page = c.block_table[size_t(w.b) * c.max_pages_per_seq + min(lp, c.max_pages_per_seq - 1)];
+          if (page < 0 || page >= c.num_pages) { atomicExch(c.status, kStatusBounds); page = 0; }
+          const int ph = page * c.n_kv + w.kvh;
+          row0 = ph * 64;
+          sk = c.k_scales[ph];
+          sv = c.v_scales[ph];
+        }
+        for (int j = 0; j < n && ok; ++j, ++it) {
+          const int st = it % kD8Stages;
+          const uint32_t ph = (it / kD8Stages) & 1;
+          const int r0 = __shfl_sync(0xffffffffu, row0, j);
+          const float skj = __shfl_sync(0xffffffffu, sk, j), svj = __shfl_sync(0xffffffffu, sv, j);
+          if (lane == 0) {
+            ok = mbar_wait(&empty[st], ph ^ 1);
+            if (ok) {
+              const float ev = c8_is_nan(svj) ? svj : float(c8_scale_exp(svj));
+              scales[st] = make_float4(skj, ev, 1.f / svj, 0.f);
+              mbar_expect_tx(&full[st], 2 * SM::kTile);
+              tma_load_2d(smem + st * 2 * SM::kTile, &tmK, &full[st], 0, r0);
+              tma_load_2d(smem + st * 2 * SM::kTile + SM::kTile, &tmV, &full[st], 0, r0);
+            }
+          }
+          ok = __shfl_sync(0xffffffffu, ok, 0);
+        }
+      }
+      dc_advance(c, w, len);
+    }
+    if (!ok && lane == 0) atomicExch(c.status, kStatusTimeout);
+    return;
+  }
+
+  // -------------------------------------------------------------------- consumers
+  const int G = c.n_q / c.n_kv;
+  const int g = lane >> 2, t4 = lane & 3;
+  const int wq = warp & 3, grp = warp >> 2;                        // quarter of a page, group of four warps
+  const int ctid = threadIdx.x;
+  // MMA row i (0..7) of a group of 8 keys is key krow(i): rows 4 apart sit in different halves of the banks
+  const int krow_g = ((g & 1) << 2) | (g >> 1);
+  const int l7 = lane & 7;
+  const int krow_l = ((l7 & 1) << 2) | (l7 >> 1);
+  const uint32_t ring = smem_u32(smem);
+  const uint32_t k_off = uint32_t(wq * 16 + krow_g) * 128 + (((t4 ^ krow_g) & 7) << 4);          // chunk t4 of the lane's first key
+  const uint32_t v_row = uint32_t(wq * 16 + ((lane >> 3) & 1) * 8 + krow_l) * 128;
+  const int v_ch = lane >> 4;                                      // ldmatrix: matrices 2 and 3 are the next chunk
+  bool ok = true;
+  int it = 0;
+
+  while (w.t < w.t_end) {
+    const int len = dc_segment_len(w);
+    const int b = w.b, kvh = w.kvh, kv_len = w.kv_len;
+    const int pair_first = w.seq_first + kvh * w.np;
+    const int c_first = pair_first / w.per;
+    const int n_segs = (pair_first + w.np - 1) / w.per - c_first + 1;
+    const int seg = int(blockIdx.x) - c_first;
+    if (w.page == 0 && kvh == 0 && ctid == 0) {
+      const int ctx = c.context_lens[b];
+      if (ctx < 0 || ctx >= c.max_len) atomicExch(c.status, kStatusBounds);
+    }
+
+    // query fragments: head g of the tile, the 16 dims of chunks t4 and t4 + 4, scaled to fp16 by a power of two
+    uint32_t qf[NT][NC][2];                                        // [tile][4 words of chunk t4, then of chunk t4 + 4][pair]
+    float qs[NT][2];                                               // log2-domain factor of heads 2 t4, 2 t4 + 1 of the tile
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      uint4 v[NC / 4][2];
+      uint32_t mx = 0;
+#pragma unroll
+      for (int hh = 0; hh < NC / 4; ++hh) {
+        const int d0 = (t4 + 4 * hh) * 16;
+        v[hh][0] = v[hh][1] = make_uint4(0, 0, 0, 0);
+        if (n * 8 + g < G && d0 < c.dh) {
+          const uint4* p = reinterpret_cast<const uint4*>(a.q + (long long)b * a.q_stride + (kvh * G + n * 8 + g) * a.q_head_stride + d0);
+          v[hh][0] = __ldg(p);
+          v[hh][1] = __ldg(p + 1);
+        }
+        mx = max(mx, max(c8_absmax(v[hh][0]), c8_absmax(v[hh][1])));
+      }
+      mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+      mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+      const int eq = c8_query_exp(mx);
+      const float down = c8_pow2(-eq);
+#pragma unroll
+      for (int hh = 0; hh < NC / 4; ++hh) {
+        const uint32_t x[8] = {v[hh][0].x, v[hh][0].y, v[hh][0].z, v[hh][0].w, v[hh][1].x, v[hh][1].y, v[hh][1].z, v[hh][1].w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) qf[n][hh * 4 + (i >> 1)][i & 1] = pack_f16(bf16_lo(x[i]) * down, bf16_hi(x[i]) * down);
+      }
+      const float f = c8_pow2(eq) * a.scale_log2;
+      qs[n][0] = __shfl_sync(0xffffffffu, f, t4 * 8);              // (lane 4 h holds head h)
+      qs[n][1] = __shfl_sync(0xffffffffu, f, t4 * 8 + 4);
+    }
+
+    float o[NT][NC][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < NC; ++i) { o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f; }
+    float m_ref[NT][2], l_run[NT][2];                              // of heads 2 t4, 2 t4 + 1; l_run: this lane's keys only
+#pragma unroll
+    for (int n = 0; n < NT; ++n) { m_ref[n][0] = m_ref[n][1] = -INFINITY; l_run[n][0] = l_run[n][1] = 0.f; }
+
+    for (int j = 0; j < len; ++j, ++it) {
+      if (CF::kGroups > 1 && (it & 1) != grp) continue;            // the other group's page
+      const int st = it % kD8Stages;
+      // A wait that runs out ends this warp's work: it keeps walking the segments (so that it still meets the other
+      // warps at every barrier and the tickets are taken) but waits for and computes nothing more.
+      if (ok && !mbar_wait(&full[st], (it / kD8Stages) & 1)) ok = false;
+      if (!ok) continue;
+      const int key0 = (w.page + j) * 64 + wq * 16;                // this warp's 16 keys of the page
+      if (key0 < kv_len) {
+        const uint32_t k_base = ring + st * 2 * SM::kTile + k_off;
+        const uint32_t v_base = ring + st * 2 * SM::kTile + SM::kTile + v_row;
+        const float4 sc = scales[st];
+        float s[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+#pragma unroll
+        for (int hh = 0; hh < NC / 4; ++hh) {
+          const uint4 x = lds128(k_base ^ (hh << 6)), y = lds128((k_base + 8 * 128) ^ (hh << 6));
+          const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t a0, a1, a2, a3;
+            c8_decode_natural<FMT>(xs[i], a0, a2);
+            c8_decode_natural<FMT>(ys[i], a1, a3);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma_f16_16816(s[n], a0, a1, a2, a3, qf[n][hh * 4 + i][0], qf[n][hh * 4 + i][1]);
+          }
+        }
+        const bool tail = key0 + 16 > kv_len;
+        bool grow = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float f = qs[n][e & 1] * sc.x;
+            const int key = key0 + krow_g + (e >> 1) * 8;
+            const bool valid = !tail || key < kv_len;
+            if (a.logits && valid && n * 8 + t4 * 2 + (e & 1) < G)
+              a.logits[(size_t(b) * c.n_q + kvh * G + n * 8 + t4 * 2 + (e & 1)) * a.logits_stride + key] = s[n][e] * f;
+            s[n][e] = valid ? fmaf(s[n][e], f, sc.y) : -INFINITY;
+          }
+          grow = grow || fmaxf(s[n][0], s[n][2]) > m_ref[n][0] + kD8Lazy || fmaxf(s[n][1], s[n][3]) > m_ref[n][1] + kD8Lazy;
+        }
+        if (__any_sync(0xffffffffu, grow)) {                       // rare after a segment's first pages
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float al[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float mx = fmaxf(s[n][e], s[n][e + 2]);
+              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+              const float m_new = fmaxf(m_ref[n][e], mx);
+              al[e] = m_ref[n][e] == -INFINITY ? 0.f : fast_exp2(m_ref[n][e] - m_new);
+              m_ref[n][e] = m_new;
+              l_run[n][e] *= al[e];
+            }
+#pragma unroll
+            for (int i = 0; i < NC; ++i) { o[n][i][0] *= al[0]; o[n][i][1] *= al[1]; o[n][i][2] *= al[0]; o[n][i][3] *= al[1]; }
+          }
+        }
+        uint32_t pb[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const float r0 = (m_ref[n][0] == -INFINITY ? 0.f : m_ref[n][0]) - kD8Shift, r1 = (m_ref[n][1] == -INFINITY ? 0.f : m_ref[n][1]) - kD8Shift;
+          const float p0 = fast_exp2(s[n][0] - r0), p1 = fast_exp2(s[n][1] - r1), p2 = fast_exp2(s[n][2] - r0), p3 = fast_exp2(s[n][3] - r1);
+          l_run[n][0] = fmaf(p0 + p2, sc.z, l_run[n][0]);
+          l_run[n][1] = fmaf(p1 + p3, sc.z, l_run[n][1]);
+          pb[n][0] = movmatrix_trans(pack_f16(p0, p1));
+          pb[n][1] = movmatrix_trans(pack_f16(p2, p3));
+        }
+        // keys behind the sequence's last one may hold anything, a NaN code included: their V codes are cleared
+        uint32_t keep0 = 0xffffffffu, keep1 = 0xffffffffu;
+        if (tail) {
+          const int i0 = t4 * 2, i1 = t4 * 2 + 1;                  // MMA key indices of this lane's halves
+          const int k0 = key0 + (((i0 & 1) << 2) | (i0 >> 1)), k1 = key0 + (((i1 & 1) << 2) | (i1 >> 1));
+          keep0 = (k0 < kv_len ? 0xffffu : 0u) | (k1 < kv_len ? 0xffff0000u : 0u);
+          keep1 = (k0 + 8 < kv_len ? 0xffffu : 0u) | (k1 + 8 < kv_len ? 0xffff0000u : 0u);
+        }
+#pragma unroll
+        for (int cp = 0; cp < NC / 2; ++cp) {
+          uint32_t v[4];
+          ldmatrix_x4_trans(v, v_base + ((((cp * 2 + v_ch) ^ krow_l) & 7) << 4));
+          if (tail) { v[0] &= keep0; v[1] &= keep1; v[2] &= keep0; v[3] &= keep1; }
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            uint32_t a0, a1, a2, a3;
+            c8_decode_split<FMT>(v[2 * u], a0, a1);
+            c8_decode_split<FMT>(v[2 * u + 1], a2, a3);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma_f16_16816(o[n][cp * 2 + u], a0, a1, a2, a3, pb[n][0], pb[n][1]);
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&empty[st]);                      // this warp is done with the stage
+    }
+
+    // ---- the warps' states become one: common maximum, then the rescaled outputs are added in a fixed order
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float l = l_run[n][e];
+        l += __shfl_xor_sync(0xffffffffu, l, 4);
+        l += __shfl_xor_sync(0xffffffffu, l, 8);
+        l += __shfl_xor_sync(0xffffffffu, l, 16);
+        if (g == 0) {
+          mm[warp * SM::kRows + n * 8 + t4 * 2 + e] = m_ref[n][e];
+          ml[warp * SM::kRows + n * 8 + t4 * 2 + e] = l;
+        }
+      }
+    d8_bar<CT>();
+    float f[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < CF::kWarps; ++q) m = fmaxf(m, mm[q * SM::kRows + n * 8 + t4 * 2 + e]);
+        f[n][e] = m_ref[n][e] == -INFINITY ? 0.f : fast_exp2(m_ref[n][e] - m);
+      }
+    // (round k: warp q adds its share of chunk (q + k) mod NC; every warp is busy in every round, no two touch the same
+    //  chunk while NC >= warps; with fewer chunks the rounds are NC apart)
+    constexpr int kRounds = NC > CF::kWarps ? NC : CF::kWarps;
+#pragma unroll 1
+    for (int k = 0; k < kRounds; ++k) {
+      const int mine = (warp + k) % kRounds;
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+        if (i != mine) continue;                                   // (o[] stays in registers: i is a compile-time index)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          // element (head, dim): the tile's row g is dim 2 g, row g + 8 dim 2 g + 1
+          float2* p0 = reinterpret_cast<float2*>(mo + (n * 8 + t4 * 2) * SM::kPitch + i * 16 + g * 2);
+          float2* p1 = reinterpret_cast<float2*>(mo + (n * 8 + t4 * 2 + 1) * SM::kPitch + i * 16 + g * 2);
+          float2 x0 = make_float2(0.f, 0.f), x1 = make_float2(0.f, 0.f);
+          // the first warp to touch chunk i is the one with (warp + k) mod kRounds == i and the smallest k: k == 0, or
+          // (fewer warps than rounds) the first k that reaches it
+          const bool first = kRounds == CF::kWarps ? k == 0 : (k == 0 || (i >= CF::kWarps && warp == CF::kWarps - 1 && k == i - warp));
+          if (!first) { x0 = *p0; x1 = *p1; }
+          x0.x += f[n][0] * o[n][i][0]; x0.y += f[n][0] * o[n][i][2];
+          x1.x += f[n][1] * o[n][i][1]; x1.y += f[n][1] * o[n][i][3];
+          *p0 = x0;
+          *p1 = x1;
+        }
+      }
+      d8_bar<CT>();
+    }
+    // row r of the segment: maximum m, sum l, unnormalised output mo[r][.]
+    auto row_ml = [&](int r, float& m, float& l) {
+      m = -INFINITY;
+      l = 0.f;
+#pragma unroll
+      for (int q = 0; q < CF::kWarps; ++q) m = fmaxf(m, mm[q * SM::kRows + r]);
+#pragma unroll
+      for (int q = 0; q < CF::kWarps; ++q) {
+        const float mq = mm[q * SM::kRows + r];
+        l += (mq == -INFINITY ? 0.f : fast_exp2(mq - m)) * ml[q * SM::kRows + r];
+      }
+    };
+    if (n_segs == 1) {
+      // the whole pair was this segment: normalise and store
+      for (int q = ctid; ok && q < G * DH; q += CT) {
+        const int r = q / DH, d = q - r * DH;
+        float m, l;
+        row_ml(r, m, l);
+        if (d < c.dh)                                              // (a 96-wide head is computed zero-padded to 128)
+          a.out[(long long)b * a.out_stride + (kvh * G + r) * c.dh + d] = __float2bfloat16_rn(mo[r * SM::kPitch + d] / l);
+        if (d == 0 && a.lse) a.lse[size_t(b) * c.n_q + kvh * G + r] = m - kD8Shift + log2f(l);
+      }
+    } else {
+      // A segment whose wait ran out writes no partial state but still takes its ticket: the counter of its pair
+      // returns to zero and the handle stays usable (this call's output is not; the status word says so).
+      const size_t slot = size_t(blockIdx.x) * 2 + (seg == 0 ? 1 : 0);
+      for (int q = ctid; ok && q < G * DH; q += CT) {
+        const int r = q / DH, d = q - r * DH;
+        a.part_o[(slot * 16 + r) * DH + d] = mo[r * SM::kPitch + d];
+        if (d == 0) {
+          float m, l;
+          row_ml(r, m, l);
+          a.part_ml[(slot * 16 + r) * 2] = m;
+          a.part_ml[(slot * 16 + r) * 2 + 1] = l;
+        }
+      }
+      __threadfence();
+      d8_bar<CT>();
+      if (ctid == 0) *ticket_s = atomicAdd(&a.split_done[b * c.n_kv + kvh], 1);
+      d8_bar<CT>();
+      if (*ticket_s == n_segs - 1) {
+        if (ctid == 0) a.split_done[b * c.n_kv + kvh] = 0;         // re-armed for the next call
+        __threadfence();
+        // One warp per query head.  The segments' (m, l) are read one per lane and their outputs eight segments at a
+        // time; the sums run in segment order.  Segment s lives in slot 1 of CTA c_first (s = 0) or slot 0 of CTA
+        // c_first + s.
+        auto slot_of = [&](int s) { return s == 0 ? size_t(c_first) * 2 + 1 : size_t(c_first + s) * 2; };
+        for (int r = warp; r < G; r += CF::kWarps) {
+          float m = -INFINITY;
+          for (int s = lane; s < n_segs; s += 32) m = fmaxf(m, __ldcg(a.part_ml + (slot_of(s) * 16 + r) * 2));
+#pragma unroll
+          for (int o2 = 16; o2 > 0; o2 >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o2));
+          float acc[DH / 32];
+#pragma unroll
+          for (int q = 0; q < DH / 32; ++q) acc[q] = 0.f;
+          float l = 0.f;
+          for (int c0 = 0; c0 < n_segs; c0 += 32) {
+            const int n = min(32, n_segs - c0);
+            float fs = 0.f, ls = 0.f;                              // lane s: factor and row sum of segment c0 + s
+            if (lane < n) {
+              const float ms = __ldcg(a.part_ml + (slot_of(c0 + lane) * 16 + r) * 2);
+              fs = ms == -INFINITY ? 0.f : fast_exp2(ms - m);
+              ls = __ldcg(a.part_ml + (slot_of(c0 + lane) * 16 + r) * 2 + 1);
+            }
+            for (int u0 = 0; u0 < n; u0 += 8) {
+              float v[8][DH / 32];
+#pragma unroll
+              for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int q = 0; q < DH / 32; ++q)
+                  v[u][q] = u0 + u < n ? __ldcg(a.part_o + (slot_of(c0 + u0 + u) * 16 + r) * DH + q * 32 + lane) : 0.f;
+#pragma unroll
+              for (int u = 0; u < 8; ++u) {
+                const float fu = __shfl_sync(0xffffffffu, fs, (u0 + u) & 31);   // (0 past the last segment)
+                const float lu = __shfl_sync(0xffffffffu, ls, (u0 + u) & 31);
+                l += fu * lu;
+#pragma unroll
+                for (int q = 0; q < DH / 32; ++q) acc[q] += fu * v[u][q];
+              }
+            }
+          }
+          const float inv = 1.f / l;
+          __nv_bfloat16* dst = a.out + (long long)b * a.out_stride + (kvh * G + r) * c.dh;
+#pragma unroll
+          for (int q = 0; q < DH / 32; ++q)
+            if (q * 32 + lane < c.dh) dst[q * 32 + lane] = __float2bfloat16_rn(acc[q] * inv);
+          if (lane == 0 && a.lse) a.lse[size_t(b) * c.n_q + kvh * G + r] = m - kD8Shift + log2f(l);
+        }
+      }
+    }
+    d8_bar<CT>();                                                  // mo, mm, ticket_s are free for the next segment
+    dc_advance(c, w, len);
+  }
+  if (!ok && lane == 0) atomicExch(c.status, kStatusTimeout);
+}
+
+// two slots of 16 rows for each CTA that can run
+size_t cache8_decode_part_rows(int n_sms) { return size_t(2) * n_sms * 2 * 16; }
+
+template <int FMT, int DH, int NT>
+static cudaError_t configure_t() {
+  return cudaFuncSetAttribute(cache8_decode_kernel<FMT, DH, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(D8Smem<DH, NT>::kBytes));
+}
+
+cudaError_t cache8_decode_configure() {
+  cudaError_t e = configure_t<kC8E4M3, 64, 1>();
+  if (e == cudaSuccess) e = configure_t<kC8E4M3, 64, 2>();
+  if (e == cudaSuccess) e = configure_t<kC8E4M3, 128, 1>();
+  if (e == cudaSuccess) e = configure_t<kC8E4M3, 128, 2>();
+  if (e == cudaSuccess) e = configure_t<kC8Int8, 64, 1>();
+  if (e == cudaSuccess) e = configure_t<kC8Int8, 64, 2>();
+  if (e == cudaSuccess) e = configure_t<kC8Int8, 128, 1>();
+  if (e == cudaSuccess) e = configure_t<kC8Int8, 128, 2>();
+  return e;
+}
+
+template <int FMT, int DH, int NT>
+static void launch_decode_t(const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a, int n_sms, cudaStream_t st) {
+  constexpr size_t smem = D8Smem<DH, NT>::kBytes;
+  static_assert(2 * (smem + 1024) <= 228 * 1024, "two CTAs per SM");
+  const long long most = ((long long)a.c.n_seqs * a.c.n_kv * a.c.max_kv_pages + kD8MinTiles - 1) / kD8MinTiles;
+  const int grid = int(most < 2LL * n_sms ? (most < 1 ? 1 : most) : 2LL * n_sms);
+  launch_pdl(cache8_decode_kernel<FMT, DH, NT>, dim3(grid), dim3(D8Cfg<NT>::kThreads), smem, st, tmK, tmV, a);
+}
+
+void launch_cache8_decode(int fmt, const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a, int n_sms, cudaStream_t st) {
+  if (a.c.n_seqs <= 0) return;
+  const bool wide = a.c.n_q / a.c.n_kv > 8, big = a.c.dh > 64;
+  if (fmt == kC8E4M3) {
+    if (big) wide ? launch_decode_t<kC8E4M3, 128, 2>(tmK, tmV, a, n_sms, st) : launch_decode_t<kC8E4M3, 128, 1>(tmK, tmV, a, n_sms, st);
+    else wide ? launch_decode_t<kC8E4M3, 64, 2>(tmK, tmV, a, n_sms, st) : launch_decode_t<kC8E4M3, 64, 1>(tmK, tmV, a, n_sms, st);
+  } else {
+    if (big) wide ? launch_decode_t<kC8Int8, 128, 2>(tmK, tmV, a, n_sms, st) : launch_decode_t<kC8Int8, 128, 1>(tmK, tmV, a, n_sms, st);
+    else wide ? launch_decode_t<kC8Int8, 64, 2>(tmK, tmV, a, n_sms, st) : launch_decode_t<kC8Int8, 64, 1>(tmK, tmV, a, n_sms, st);
+  }
+}
+
+}  // namespace foe

@@ -1,0 +1,616 @@
+// Attention of prompt chunks over the 8-bit cache on the 5th-generation tensor cores.
+//
+// The structure is that of the bf16 prefill kernel (attention_tc.cu): one CTA owns 128 query rows of two query heads that
+// share a KV head, S = Q K^T and O += P V as tcgen05.mma with S, P and O in tensor memory, two softmax threads per query
+// row that take the 64-key steps in turn, and a running maximum that moves only by more than 2^8.  What the 8-bit cache
+// changes:
+//   * K and V pages arrive as codes (TMA, half the bytes) and four converter warps turn them into fp16 operand tiles
+//     in the 128-byte-swizzled layout, exactly and unscaled.  The page's K scale multiplies the scores and its V scale
+//     enters the exponent, t = s + log2(scale_v); the row sum takes it back out.
+//   * Q becomes fp16 once per CTA: a power of two per row brings the row's largest element to [2^7, 2^8), which keeps
+//     every bf16 value within 2^31 of it (the factor joins the K scale).  P is fp16 too (11 bits where bf16 has 8),
+//     kept 2^6 above its natural scale so that only probabilities below 2^-30 of the largest are lost.
+//   * K and V tiles have rings of their own: a K tile is free as soon as its scores exist, so the converters run ahead.
+//   * Calls with few query rows split the keys over CTAs; each split leaves (m, l, unnormalised O) and a second kernel
+//     joins them in order.
+// Warp roles (768 threads): warp 0 TMA producer, warps 1 and 2 MMA issuers (one per head), warps 4-7 converters, warps
+// 8-23 softmax.
+#include <math.h>
+
+#include "attention_tc.cuh"
+#include "cache8.cuh"
+#include "cache8.h"
+
+namespace foe {
+
+constexpr int kC8Rows = 128, kC8Keys = 64;
+constexpr int kC8Threads = 768;
+constexpr int kC8Raw = 3, kC8Ring = 3;            // stages of codes; operand tiles of K and of V
+constexpr int kC8Scales = 16;                     // ring of the steps' scales (further ahead than the producer can be)
+constexpr int kC8SoftWarp = 8;                    // first softmax warp
+// Registers: the block is launched with kC8RegsLaunch each; warpgroup 0 and the converters hand back what the four
+// softmax warpgroups take (setmaxnreg.inc would wait forever for more than that).
+constexpr int kC8RegsLaunch = 80, kC8RegsLow = 24, kC8RegsConv = 40, kC8RegsHigh = 104;
+static_assert(128 * (kC8RegsLow + kC8RegsConv) + 512 * kC8RegsHigh <= kC8Threads * kC8RegsLaunch, "softmax warpgroups would wait for registers forever");
+constexpr float kC8Shift = 6.f;
+
+__device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// fp16 x fp16 -> fp32, M x N tile, both operands K-major
+__host__ __device__ constexpr uint32_t umma_idesc_f16(int M, int N) {
+  return (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
+}
+
+template <int DH>
+struct C8Smem {
+  static constexpr int kQTile = kC8Rows * DH * 2;
+  static constexpr int kTile = kC8Keys * DH * 2;               // one fp16 operand tile
+  static constexpr int kRawTile = kC8Keys * 128;               // codes, rows padded to 128 bytes by the TMA box
+  static constexpr int kQOff = 0;
+  static constexpr int kKOff = 2 * kQTile;
+  static constexpr int kVOff = kKOff + kC8Ring * kTile;
+  static constexpr int kRawOff = kVOff + kC8Ring * kTile;
+  static constexpr int kBarOff = kRawOff + kC8Raw * 2 * kRawTile;
+  static constexpr int kScaleOff = kBarOff + 384;              // [kC8Scales] (K scale, log2 V scale, 1 / V scale, -)
+  static constexpr int kHandOff = kScaleOff + kC8Scales * 16;  // [2 tiles][128 rows][2]
+  static constexpr int kRedOff = kHandOff + 2 * kC8Rows * 2 * 4;
+  static constexpr size_t kBytes = kRedOff + 128 + 1024;
+};
+
+// query heads a CTA works on: two that share a KV head, or one where the group is odd
+__device__ __forceinline__ int c8_heads_per_block(const Cache8Args& c) { return (c.n_q / c.n_kv) % 2 == 0 ? 2 : 1; }
+
+template <int FMT, int DH>
+__global__ void __launch_bounds__(kC8Threads, 1)
+cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const Cache8AttendArgs a,
+                    const int q_blocks, const int n_splits) {
+  pdl_wait();
+  pdl_launch_dependents();
+  using L = C8Smem<DH>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBarOff);
+  uint64_t* q_full = bars;                         // 2 tiles: the tile's eight softmax warps have written their query rows
+  uint64_t* raw_full = bars + 2;                   // kC8Raw
+  uint64_t* raw_empty = raw_full + kC8Raw;
+  uint64_t* k_full = raw_empty + kC8Raw;           // kC8Ring: four converter warps
+  uint64_t* k_empty = k_full + kC8Ring;
+  uint64_t* v_full = k_empty + kC8Ring;
+  uint64_t* v_empty = v_full + kC8Ring;
+  uint64_t* s_full = v_empty + kC8Ring;            // 2 tiles: the scores are in tensor memory (the commit and a plain arrival)
+  uint64_t* s_free = s_full + 2;
+  uint64_t* p_ready = s_free + 2;
+  uint64_t* o_full = p_ready + 2;                  // 2 tiles x 2 step parities
+  uint64_t* o_done = o_full + 4;
+  uint64_t* hand = o_done + 2;                     // 2 tiles x 4 lane quarters
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(hand + 8);
+  static_assert((2 + 2 * kC8Raw + 4 * kC8Ring + 12 + 8 + 1) * 8 <= 384, "barriers");
+  float4* scales = reinterpret_cast<float4*>(smem + L::kScaleOff);
+  int* red = reinterpret_cast<int*>(smem + L::kRedOff);
+  const Cache8Args& c = a.c;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // Blocks start in the order of their linear index: late query blocks (long causal extents) of the whole call first.
+  const int n_tiles_q = c8_heads_per_block(c);
+  const int pairs = c.n_q / n_tiles_q;
+  const int split = blockIdx.x % n_splits;
+  const int lin = blockIdx.x / n_splits;
+  const int per_qb = pairs * c.n_seqs;
+  const int qb = q_blocks - 1 - lin / per_qb;
+  const int pair = (lin % per_qb) % pairs;
+  const int b = (lin % per_qb) / pairs;
+  const int head0 = pair * n_tiles_q;
+  const int kvh = head0 / (c.n_q / c.n_kv);
+  const int q_len = c.q_lens ? c.q_lens[b] : 1;
+  const int ctx = c.context_lens[b];
+  const int q0 = qb * kC8Rows;
+  const bool bad = q_len < 0 || q_len > c.max_q_len || ctx < 0 || (long long)ctx + q_len > c.max_len;
+  if (!bad && q0 >= q_len) return;
+  const int start = c.q_lens ? c8_block_prefix(c.q_lens, b, red) : b;
+  if (bad || (long long)start + q_len > c.n_tokens) {     // lengths that disagree with what the host was told
+    if (threadIdx.x == 0) atomicExch(c.status, kStatusBounds);
+    return;
+  }
+  const int tok0 = start + q0;
+  const int rows_here = min(kC8Rows, q_len - q0);
+  const int kv_len = ctx + q0 + rows_here;
+  const int all_steps = (kv_len + kC8Keys - 1) / kC8Keys;
+  const int per_split = (all_steps + n_splits - 1) / n_splits;
+  const int step0 = split * per_split;
+  const int n_steps = min(all_steps - step0, per_split);
+  if (n_steps <= 0) return;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kC8Raw; ++s) { mbar_init(&raw_full[s], 1); mbar_init(&raw_empty[s], 4); }
+    for (int s = 0; s < kC8Ring; ++s) {
+      mbar_init(&k_full[s], 4); mbar_init(&k_empty[s], n_tiles_q);
+      mbar_init(&v_full[s], 4); mbar_init(&v_empty[s], n_tiles_q);
+    }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(&q_full[t], 8);
+      mbar_init(&s_full[t], 2); mbar_init(&s_free[t], 4); mbar_init(&p_ready[t], 4);
+      mbar_init(&o_full[2 * t], 1); mbar_init(&o_full[2 * t + 1], 1);
+      mbar_init(&o_done[t], 1);
+      for (int q = 0; q < 4; ++q) mbar_init(&hand[4 * t + q], 1);
+    }
+    mbar_fence_init();
+    tma_prefetch_desc(&tmK); tma_prefetch_desc(&tmV);
+  }
+  if (warp == 1) { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  // tensor-memory columns of tile t: scores at 128 t, P of step parity b at 128 t + 64 + 32 b; O at 256 + DH t
+  const uint32_t q_u32 = smem_u32(smem + L::kQOff), k_u32 = smem_u32(smem + L::kKOff), v_u32 = smem_u32(smem + L::kVOff);
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kC8RegsLow));
+    if (warp == 0) {
+      // ---------------------------------------------------------------- TMA producer
+      if (elect_one()) {
+        bool ok = true;
+        for (int j = 0; j < n_steps && ok; ++j) {
+          const int s = j % kC8Raw;
+          if (!mbar_wait(&raw_empty[s], ((j / kC8Raw) & 1) ^ 1)) { ok = false; break; }
+          int page = c.block_table[size_t(b) * c.max_pages_per_seq + step0 + j];
+          if (page < 0 || page >= c.num_pages) { atomicExch(c.status, kStatusBounds); page = 0; }
+          const int ph = page * c.n_kv + kvh;
+          const float sk = c.k_scales[ph], sv = c.v_scales[ph];
+          scales[j % kC8Scales] = make_float4(sk, c8_is_nan(sv) ? sv : float(c8_scale_exp(sv)), 1.f / sv, 0.f);
+          uint8_t* dst = smem + L::kRawOff + s * 2 * L::kRawTile;
+          mbar_expect_tx(&raw_full[s], 2 * L::kRawTile);
+          tma_load_2d(dst, &tmK, &raw_full[s], 0, ph * kC8Keys);
+          tma_load_2d(dst + L::kRawTile, &tmV, &raw_full[s], 0, ph * kC8Keys);
+        }
+        if (!ok) atomicExch(c.status, kStatusTimeout);
+      }
+    } else if (warp == 1 || warp == 2) {
+      // ---------------------------------------------------------------- MMA issuers, one per tile
+      const int t = warp - 1;
+      if (t < n_tiles_q && elect_one()) {
+        constexpr uint32_t idesc_s = umma_idesc_f16(kC8Rows, kC8Keys);
+        constexpr uint32_t idesc_o = umma_idesc_f16(kC8Rows, DH) | (1u << 16);       // B operand (V) is MN-major
+        bool ok = mbar_wait(&q_full[t], 0);
+        int q = 0, p = 0;                                                 // next Q K^T, next P V
+        unsigned long long t0 = 0;
+        for (uint32_t spin = 0; p < n_steps && ok;) {
+          bool did = false;
+          if (q < n_steps && mbar_test(&k_full[q % kC8Ring], (q / kC8Ring) & 1) && (q == 0 || mbar_test(&s_free[t], (q - 1) & 1))) {
+            tc_fence_after();
+            const uint32_t qb_ = q_u32 + t * L::kQTile, kb_ = k_u32 + (q % kC8Ring) * L::kTile;
+#pragma unroll
+            for (int ks = 0; ks < DH / 16; ++ks) {
+              const uint32_t off_q = (ks >> 2) * (kC8Rows * 128) + (ks & 3) * 32;
+              const uint32_t off_k = (ks >> 2) * (kC8Keys * 128) + (ks & 3) * 32;
+              umma_bf16(tmem_base + t * 128, desc_kmajor(qb_ + off_q), desc_kmajor(kb_ + off_k), idesc_s, ks != 0);
+            }
+            umma_commit(&s_full[t]);
+            umma_commit(&k_empty[q % kC8Ring]);
+            mbar_arrive(&s_full[t]);             // carries the producer's writes (the step's scales) on to the softmax threads
+            ++q;
+            did = true;
+          }
+          if (p < q && mbar_test(&p_ready[t], p & 1) && mbar_test(&v_full[p % kC8Ring], (p / kC8Ring) & 1)) {
+            tc_fence_after();
+            const uint32_t p_tmem = tmem_base + t * 128 + 64 + (p & 1) * 32, vb_ = v_u32 + (p % kC8Ring) * L::kTile;
+#pragma unroll
+            for (int kk = 0; kk < kC8Keys / 16; ++kk)
+              umma_bf16_ts(tmem_base + 256 + t * DH, p_tmem + kk * 8, desc_mnmajor(vb_ + kk * (16 * 128), kC8Keys * 128, 1024),
+                           idesc_o, (p | kk) != 0);
+            umma_commit(&o_full[2 * t + (p & 1)]);
+            umma_commit(&v_empty[p % kC8Ring]);
+            ++p;
+            did = true;
+          }
+          if (did) { spin = 0; t0 = 0; continue; }
+          if ((++spin & 0x3ff) == 0) {                                    // bounded like every other wait
+            const unsigned long long now = globaltimer_ns();
+            if (t0 == 0) t0 = now;
+            else if (now - t0 > kWaitLimitNs) ok = false;
+          }
+        }
+        umma_commit(&o_done[t]);                                          // (also after a timeout: nobody waits in vain)
+        if (!ok) atomicExch(c.status, kStatusTimeout);
+      }
+    }
+  } else if (warp < kC8SoftWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kC8RegsConv));
+    // ------------------------------------------------------------------ converters: codes -> fp16 operand tiles
+    // A thread takes 16 codes of a row at a time; its 32 bytes of fp16 go to two 16-byte chunks of the row's 128-byte
+    // line in the 64-column half they belong to.  Lanes of the upper half write their chunks in the other order, so that
+    // eight lanes (one row) always hit eight different chunks.
+    const int tid = threadIdx.x - 128;
+    constexpr int CH = DH / 16;
+    bool ok = true;
+    auto convert = [&](const uint8_t* src, uint8_t* dst, int valid_rows) {
+#pragma unroll 2
+      for (int p = tid; p < kC8Keys * CH; p += 128) {
+        const int row = p / CH, ch = p % CH;
+        uint4 x = *reinterpret_cast<const uint4*>(src + row * 128 + (((ch ^ row) & 7) << 4));
+        if (row >= valid_rows) x = make_uint4(0, 0, 0, 0);
+        uint4 u, v;
+        c8_decode_natural<FMT>(x.x, u.x, u.y);
+        c8_decode_natural<FMT>(x.y, u.z, u.w);
+        c8_decode_natural<FMT>(x.z, v.x, v.y);
+        c8_decode_natural<FMT>(x.w, v.z, v.w);
+        uint8_t* line = dst + (ch >> 2) * (kC8Keys * 128) + row * 128;
+        const int c0 = (ch & 3) * 2, flip = (ch >> 2) & 1;
+        *reinterpret_cast<uint4*>(line + (((c0 + flip) ^ (row & 7)) << 4)) = flip ? v : u;
+        *reinterpret_cast<uint4*>(line + (((c0 + 1 - flip) ^ (row & 7)) << 4)) = flip ? u : v;
+      }
+    };
+    for (int j = 0; j < n_steps; ++j) {
+      const int s = j % kC8Raw, r = j % kC8Ring;
+      const uint32_t ph = (j / kC8Ring) & 1;
+      const uint8_t* src = smem + L::kRawOff + s * 2 * L::kRawTile;
+      if (!mbar_wait(&raw_full[s], (j / kC8Raw) & 1) || !mbar_wait(&k_empty[r], ph ^ 1)) { ok = false; break; }
+      convert(src, smem + L::kKOff + r * L::kTile, kC8Keys);
+      fence_proxy_async();                                   // the tensor core reads these through the async proxy
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&k_full[r]);
+      if (!mbar_wait(&v_empty[r], ph ^ 1)) { ok = false; break; }
+      // rows behind the block's last key may hold anything, a NaN code included, and their P is zero
+      convert(src + L::kRawTile, smem + L::kVOff + r * L::kTile, min(kC8Keys, kv_len - (step0 + j) * kC8Keys));
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) { mbar_arrive(&v_full[r]); mbar_arrive(&raw_empty[s]); }
+    }
+    if (!ok && lane == 0) atomicExch(c.status, kStatusTimeout);
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kC8RegsHigh));
+    // ------------------------------------------------------------------ softmax, two threads per query row
+    const int grp = (warp - kC8SoftWarp) >> 2;               // four consecutive warps cover the four lane quarters
+    const int t = grp >> 1;                                  // tile of this warp group
+    const int g = grp & 1;                                   // this thread takes the steps j with j % 2 == g
+    if (t < n_tiles_q) {
+      const int quarter = warp & 3;
+      const int row = quarter * 32 + lane;                   // row of the tile = TMEM lane
+      const uint32_t lane_sel = static_cast<uint32_t>(quarter * 32) << 16;
+      const uint32_t s_base = tmem_base + lane_sel + t * 128;
+      const uint32_t p_base = s_base + 64;
+      const uint32_t o_addr = tmem_base + lane_sel + 256 + t * DH;
+      const int qpos = ctx + q0 + row;
+      const int first_mask_step = (ctx + q0) / kC8Keys - step0;
+      const int pair_bar = 1 + t * 4 + quarter;              // the two warps that own these 32 rows
+      float* m_hand = reinterpret_cast<float*>(smem + L::kHandOff) + (t * kC8Rows + row) * 2;
+      uint64_t* hand_bar = &hand[4 * t + quarter];
+
+      // ---- the row of Q: each of its two threads takes half of the columns
+      float rf;                                              // log2-domain factor of the row's scores
+      {
+        constexpr int QC = DH / 16;                          // 8-element chunks of a thread
+        uint4 v[QC];
+        uint32_t mx = 0;
+        const __nv_bfloat16* src = a.q + (long long)(tok0 + row) * a.q_stride + (head0 + t) * a.q_head_stride + g * (DH / 2);
+#pragma unroll
+        for (int i = 0; i < QC; ++i) {
+          v[i] = make_uint4(0, 0, 0, 0);
+          if (row < rows_here && g * (DH / 2) + i * 8 < c.dh) v[i] = __ldg(reinterpret_cast<const uint4*>(src + i * 8));
+          mx = max(mx, c8_absmax(v[i]));
+        }
+        m_hand[g] = __uint_as_float(mx);
+        named_barrier(pair_bar, 64);
+        mx = max(mx, __float_as_uint(m_hand[g ^ 1]));
+        const int eq = c8_query_exp(mx);
+        const float down = c8_pow2(-eq);
+        rf = c8_pow2(eq) * a.scale_log2;
+        uint8_t* qt = smem + L::kQOff + t * L::kQTile;
+#pragma unroll
+        for (int i = 0; i < QC; ++i) {
+          const int ch = g * QC + i;                         // chunk of the row
+          const uint4 h = make_uint4(pack_f16(bf16_lo(v[i].x) * down, bf16_hi(v[i].x) * down), pack_f16(bf16_lo(v[i].y) * down, bf16_hi(v[i].y) * down),
+                                     pack_f16(bf16_lo(v[i].z) * down, bf16_hi(v[i].z) * down), pack_f16(bf16_lo(v[i].w) * down, bf16_hi(v[i].w) * down));
+          *reinterpret_cast<uint4*>(qt + (ch >> 3) * (kC8Rows * 128) + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) = h;
+        }
+        fence_proxy_async();
+        named_barrier(pair_bar, 64);                         // (both threads have read the other's maximum: m_hand is free)
+        if (lane == 0) mbar_arrive(&q_full[t]);
+      }
+
+      // m_ref: the (possibly stale) maximum the exponentials of the row use, the same in both of its threads at every
+      // step; l_run: sum of the probabilities of THIS thread's steps, kept relative to m_ref
+      float m_ref = -INFINITY, l_run = 0.f;
+      bool ok = true;
+      for (int j = g; j < n_steps; j += 2) {
+        const uint32_t ph = j & 1;
+        const bool masked = j >= first_mask_step;
+        // (the other thread's reference first: it also keeps the parity wait on the scores sound, see attention_tc.cu)
+        if (j > 0) {
+          if (!mbar_wait(hand_bar, ph ^ 1)) { ok = false; break; }
+          const float m_prev = *m_hand;
+          if (m_prev != m_ref) {
+            l_run *= (m_ref == -INFINITY) ? 0.f : fast_exp2(m_ref - m_prev);
+            m_ref = m_prev;
+          }
+        }
+        uint32_t r0[32], r1[32];                             // the 64 scores of this row
+        if (!mbar_wait(&s_full[t], ph)) { ok = false; break; }
+        tc_fence_after();
+        tmem_ld32(s_base, r0);                               // two loads in flight, one wait
+        tmem_ld32(s_base + 32, r1);
+        const float4 sc4 = scales[j % kC8Scales];
+        const float sc = rf * sc4.x;
+        tmem_ld_wait();
+        tc_fence_before();                                   // the scores are in registers: the buffer may take step j+1
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s_free[t]);
+        if (masked) {
+          const int k0 = (step0 + j) * kC8Keys;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            if (k0 + i > qpos) r0[i] = 0xff800000u;          // -inf: key after the query
+            if (k0 + 32 + i > qpos) r1[i] = 0xff800000u;
+          }
+        }
+        float mx;
+        {                                                    // four independent chains, then a short tree
+          float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              m4[q] = fmax3(m4[q], __uint_as_float(r0[i + q]), __uint_as_float(r1[i + q]));
+          }
+          mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+        }
+        const float m_new = fmaxf(m_ref, fmaf(mx, sc, sc4.y));
+        // move the reference maximum (and rescale O) only when it is off by more than 2^8; warp-uniform so that
+        // the tensor-memory accesses stay aligned
+        const bool move = __any_sync(0xffffffffu, m_new > m_ref + 8.0f);
+        // publish this step's reference at once: the other thread needs nothing else to start its exponentials
+        *m_hand = move ? m_new : m_ref;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(hand_bar);
+        // the completion of the previous step's P V product is observed exactly once per step (see attention_tc.cu)
+        bool o_seen = (j == 0);
+        if (move) {
+          const float alpha = (m_ref == -INFINITY) ? 0.f : fast_exp2(m_ref - m_new);
+          if (j > 0) {
+            if (!mbar_wait(&o_full[2 * t + (ph ^ 1)], ((j - 1) >> 1) & 1)) { ok = false; break; }   // every P V product so far has landed
+            o_seen = true;
+            tc_fence_after();
+#pragma unroll 1
+            for (int c8 = 0; c8 < DH / 8; ++c8) {
+              uint32_t r[8];
+              tmem_ld8(o_addr + c8 * 8, r);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
+              tmem_st8(o_addr + c8 * 8, r);
+            }
+            tmem_st_wait();
+          }
+          l_run *= alpha;
+          m_ref = m_new;
+        }
+        const float off = sc4.y + kC8Shift - ((m_ref == -INFINITY) ? 0.f : m_ref);
+        // probabilities, written as the fp16 A operand of the PV product (exp2(-inf) = 0 handles the mask)
+        const uint32_t p_addr = p_base + (j & 1) * 32;
+        if (j >= 2 && !mbar_wait(&o_full[2 * t + ph], ((j - 2) >> 1) & 1)) { ok = false; break; }   // P V of step j-2 has read this buffer
+        uint64_t rs2[4] = {0ull, 0ull, 0ull, 0ull};           // four independent chains of (even, odd) partial sums
+        const uint64_t sc2 = pack_f32x2(sc, sc), of2 = pack_f32x2(off, off);
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          uint32_t (&rr)[32] = (q4 < 2) ? r0 : r1;
+          const int c0 = (q4 & 1) * 16;
+          float e[16];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const uint64_t v = fma_f32x2(pack_b32x2(rr[c0 + 2 * i], rr[c0 + 2 * i + 1]), sc2, of2);
+            unpack_f32x2(v, e[2 * i], e[2 * i + 1]);
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(e[i]) : "f"(e[i]));
+          uint32_t pk[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            rs2[i & 3] = add_f32x2(rs2[i & 3], pack_f32x2(e[2 * i], e[2 * i + 1]));
+            pk[i] = pack_f16(e[2 * i], e[2 * i + 1]);
+          }
+          tmem_st8(p_addr + q4 * 8, pk);
+        }
+        float rs4[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) { float lo, hi; unpack_f32x2(rs2[q], lo, hi); rs4[q] = lo + hi; }
+        l_run = fmaf((rs4[0] + rs4[1]) + (rs4[2] + rs4[3]), sc4.z, l_run);
+        if (!o_seen && !mbar_wait(&o_full[2 * t + (ph ^ 1)], ((j - 1) >> 1) & 1)) { ok = false; break; }
+        tmem_st_wait();                                      // P is in tensor memory
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_ready[t]);
+      }
+      if (ok) ok = mbar_wait(&o_done[t], 0);                 // every product of the block has completed
+      tc_fence_after();
+      if (!ok && lane == 0) atomicExch(c.status, kStatusTimeout);
+      // The row's two threads meet here through four columns of the tile's score buffer in tensor memory: each leaves
+      // the reference it last knew and its partial sum.  Both warps of a row reach this barrier whatever happened before
+      // (every wait above is bounded).
+      tmem_st1(s_base + 2 * g, __float_as_uint(m_ref));
+      tmem_st1(s_base + 2 * g + 1, __float_as_uint(l_run));
+      tmem_st_wait();
+      tc_fence_before();
+      named_barrier(pair_bar, 64);
+      tc_fence_after();
+      float m_fin = -INFINITY, l_fin = 0.f;
+      if (ok) {
+        // the reference only ever grows and O is scaled to its last value, the larger of the two
+        const float m_o = __uint_as_float(tmem_ld1(s_base + 2 * (g ^ 1)));
+        const float l_o = __uint_as_float(tmem_ld1(s_base + 2 * (g ^ 1) + 1));
+        m_fin = fmaxf(m_ref, m_o);
+        // (a sum whose reference never moved from -inf is zero, or NaN where a page's scale is)
+        const float l_mine = l_run * ((m_ref == m_fin) ? 1.f : (m_ref == -INFINITY ? 0.f : fast_exp2(m_ref - m_fin)));
+        const float l_oth = l_o * ((m_o == m_fin) ? 1.f : (m_o == -INFINITY ? 0.f : fast_exp2(m_o - m_fin)));
+        l_fin = g ? l_oth + l_mine : l_mine + l_oth;         // same order in both threads
+      }
+      if (n_splits > 1) {
+        // partial result of the split: the row's (m, l) and its unnormalised output, half of the columns per thread
+        if (ok && row < rows_here) {
+          const size_t prow = (size_t(blockIdx.x) * 2 + t) * kC8Rows + row;
+          if (g == 0) { a.part_ml[prow * 2] = m_fin; a.part_ml[prow * 2 + 1] = l_fin; }
+        }
+        if (ok) {
+          const size_t prow = (size_t(blockIdx.x) * 2 + t) * kC8Rows + row;
+#pragma unroll
+          for (int cq = 0; cq < DH / 64; ++cq) {
+            const int ch = g * (DH / 64) + cq;
+            uint32_t r[32];
+            tmem_ld32(o_addr + ch * 32, r);
+            tmem_ld_wait();
+            if (row < rows_here) {
+              uint4* dst = reinterpret_cast<uint4*>(a.part_o + prow * DH + ch * 32);
+#pragma unroll
+              for (int q = 0; q < 8; ++q) dst[q] = make_uint4(r[4 * q], r[4 * q + 1], r[4 * q + 2], r[4 * q + 3]);
+            }
+          }
+        }
+      } else {
+        // Normalise: the pair stages its 32 rows in its slice of the (no longer needed) query tile, each thread half of
+        // the row's columns; after a barrier each warp stores 16 of the rows whole.
+        uint8_t* stg = smem + L::kQOff + t * L::kQTile + quarter * 32 * (DH * 2);
+        if (ok) {
+          const float inv_l = 1.f / l_fin;
+          if (g == 0 && a.lse && row < rows_here) a.lse[size_t(tok0 + row) * c.n_q + head0 + t] = m_fin - kC8Shift + log2f(l_fin);
+#pragma unroll
+          for (int cq = 0; cq < DH / 64; ++cq) {
+            const int ch = g * (DH / 64) + cq;
+            uint32_t r[32];
+            tmem_ld32(o_addr + ch * 32, r);
+            tmem_ld_wait();
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const int cc = ch * 4 + q;
+              uint4 v = make_uint4(pack_bf16(__uint_as_float(r[8 * q]) * inv_l, __uint_as_float(r[8 * q + 1]) * inv_l),
+                                   pack_bf16(__uint_as_float(r[8 * q + 2]) * inv_l, __uint_as_float(r[8 * q + 3]) * inv_l),
+                                   pack_bf16(__uint_as_float(r[8 * q + 4]) * inv_l, __uint_as_float(r[8 * q + 5]) * inv_l),
+                                   pack_bf16(__uint_as_float(r[8 * q + 6]) * inv_l, __uint_as_float(r[8 * q + 7]) * inv_l));
+              *reinterpret_cast<uint4*>(stg + lane * (DH * 2) + ((cc ^ (lane & 7)) << 4)) = v;
+            }
+          }
+        }
+        named_barrier(pair_bar, 64);
+        if (ok) {
+          constexpr int CH = DH / 8;                         // 16-byte chunks per row
+          constexpr int RPI = 32 / CH;                       // rows per store instruction
+          for (int r0 = g * 16; r0 < g * 16 + 16; r0 += RPI) {
+            const int rr = r0 + lane / CH, cc = lane % CH;
+            const int grow = quarter * 32 + rr;
+            if (grow < rows_here && cc * 8 < c.dh)           // (a 96-wide head is computed zero-padded to 128)
+              *reinterpret_cast<uint4*>(a.out + (long long)(tok0 + grow) * a.out_stride + (head0 + t) * c.dh + cc * 8) =
+                  *reinterpret_cast<const uint4*>(stg + rr * (DH * 2) + ((cc ^ (rr & 7)) << 4));
+          }
+        }
+      }
+    }
+  }
+
+  // ---------------------------------------------------------------------- teardown
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, 512);
+  }
+}
+
+// Joins the splits of a call: one warp per (query row, head) of a block, splits in order.
+constexpr int kC8JoinThreads = 256;
+template <int DH>
+__global__ void __launch_bounds__(kC8JoinThreads)
+cache8_join_kernel(const Cache8AttendArgs a, const int q_blocks, const int n_splits) {
+  pdl_wait();
+  pdl_launch_dependents();
+  __shared__ int red[kC8JoinThreads / 32];
+  const Cache8Args& c = a.c;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n_tiles_q = c8_heads_per_block(c);
+  const int pairs = c.n_q / n_tiles_q;
+  const int lin = blockIdx.x, t = blockIdx.y;
+  const int per_qb = pairs * c.n_seqs;
+  const int qb = q_blocks - 1 - lin / per_qb;
+  const int pair = (lin % per_qb) % pairs;
+  const int b = (lin % per_qb) / pairs;
+  const int head = pair * n_tiles_q + t;
+  const int q_len = c.q_lens ? c.q_lens[b] : 1;
+  const int ctx = c.context_lens[b];
+  const int q0 = qb * kC8Rows;
+  if (q_len < 0 || q_len > c.max_q_len || ctx < 0 || (long long)ctx + q_len > c.max_len || q0 >= q_len) return;
+  const int start = c.q_lens ? c8_block_prefix(c.q_lens, b, red) : b;
+  if ((long long)start + q_len > c.n_tokens) return;
+  const int rows_here = min(kC8Rows, q_len - q0);
+  const int all_steps = (ctx + q0 + rows_here + kC8Keys - 1) / kC8Keys;
+  const int per_split = (all_steps + n_splits - 1) / n_splits;
+  const int used = (all_steps + per_split - 1) / per_split;
+  for (int row = blockIdx.z * (kC8JoinThreads / 32) + warp; row < rows_here; row += gridDim.z * (kC8JoinThreads / 32)) {
+    auto prow = [&](int s) { return ((size_t(lin) * n_splits + s) * 2 + t) * kC8Rows + row; };
+    float m = -INFINITY;
+    for (int s = lane; s < used; s += 32) m = fmaxf(m, a.part_ml[prow(s) * 2]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    float acc[DH / 32], l = 0.f;
+#pragma unroll
+    for (int q = 0; q < DH / 32; ++q) acc[q] = 0.f;
+    for (int s = 0; s < used; ++s) {
+      const float ms = a.part_ml[prow(s) * 2], ls = a.part_ml[prow(s) * 2 + 1];
+      const float f = ms == m ? 1.f : (ms == -INFINITY ? 0.f : fast_exp2(ms - m));
+      l += f * ls;
+#pragma unroll
+      for (int q = 0; q < DH / 32; ++q) acc[q] += f * a.part_o[prow(s) * DH + q * 32 + lane];
+    }
+    const float inv = 1.f / l;
+    __nv_bfloat16* dst = a.out + (long long)(start + q0 + row) * a.out_stride + head * c.dh;
+#pragma unroll
+    for (int q = 0; q < DH / 32; ++q)
+      if (q * 32 + lane < c.dh) dst[q * 32 + lane] = __float2bfloat16_rn(acc[q] * inv);
+    if (lane == 0 && a.lse) a.lse[size_t(start + q0 + row) * c.n_q + head] = m - kC8Shift + log2f(l);
+  }
+}
+
+template <int FMT, int DH>
+static cudaError_t configure_t() {
+  cudaFuncAttributes fa;
+  cudaError_t e = cudaFuncGetAttributes(&fa, cache8_chunk_kernel<FMT, DH>);
+  if (e != cudaSuccess) return e;
+  // the register hand-over inside the kernel assumes this many at launch; anything else is refused here
+  if (fa.numRegs != kC8RegsLaunch) return cudaErrorInvalidConfiguration;
+  return cudaFuncSetAttribute(cache8_chunk_kernel<FMT, DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(C8Smem<DH>::kBytes));
+}
+
+cudaError_t cache8_chunk_configure() {
+  cudaError_t e = configure_t<kC8E4M3, 64>();
+  if (e == cudaSuccess) e = configure_t<kC8E4M3, 128>();
+  if (e == cudaSuccess) e = configure_t<kC8Int8, 64>();
+  if (e == cudaSuccess) e = configure_t<kC8Int8, 128>();
+  return e;
+}
+
+size_t cache8_chunk_part_rows(int n_sms) { return size_t(n_sms) * 2 * kC8Rows; }
+
+template <int FMT, int DH>
+static int launch_chunk_t(const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a, int n_sms, cudaStream_t st) {
+  const Cache8Args& c = a.c;
+  const int tiles = (c.n_q / c.n_kv) % 2 == 0 ? 2 : 1;
+  const int q_blocks = (c.max_q_len + kC8Rows - 1) / kC8Rows;
+  const long long blocks = (long long)q_blocks * (c.n_q / tiles) * c.n_seqs;
+  // one CTA per SM: a call that fills less than half of them splits its keys, at least 4 pages (and a CTA's start-up and
+  // the joining pass) a split
+  int splits = int(blocks < 1 ? 1 : n_sms / blocks);
+  const int most = (c.max_kv_pages + 3) / 4;
+  if (splits > most) splits = most;
+  if (splits < 1) splits = 1;
+  launch_pdl(cache8_chunk_kernel<FMT, DH>, dim3(unsigned(blocks * splits)), dim3(kC8Threads), size_t(C8Smem<DH>::kBytes), st, tmK, tmV, a, q_blocks, splits);
+  if (splits > 1) {
+    const int z = c.max_q_len < kC8Rows ? (c.max_q_len + 7) / 8 : kC8Rows / 8;
+    launch_pdl(cache8_join_kernel<DH>, dim3(unsigned(blocks), tiles, z), dim3(kC8JoinThreads), 0, st, a, q_blocks, splits);
+  }
+  return splits > 1 ? 2 : 1;
+}
+
+int launch_cache8_chunk(int fmt, const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a, int n_sms, cudaStream_t st) {
+  if (a.c.n_seqs <= 0 || a.c.n_tokens <= 0) return 0;
+  if (fmt == kC8E4M3) {
+    return a.c.dh > 64 ? launch_chunk_t<kC8E4M3, 128>(tmK, tmV, a, n_sms, st) : launch_chunk_t<kC8E4M3, 64>(tmK, tmV, a, n_sms, st);
+  }
+  return a.c.dh > 64 ? launch_chunk_t<kC8Int8, 128>(tmK, tmV, a, n_sms, st) : launch_chunk_t<kC8Int8, 64>(tmK, tmV, a, n_sms, st);
+}
+
+}  // namespace foe

@@ -9,27 +9,13 @@
 
 #include "../../include/foe.h"
 #include "../../include/foe_shard.h"
+#include "cache8_handle.h"
 #include "kernels.h"
+#include "tensor_map.h"
 
 using namespace foe;
 
 namespace {
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn get_encode_fn() {
-  static EncodeTiledFn fn = nullptr;
-  if (!fn) {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult qres;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess &&
-        qres == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeTiledFn>(p);
-  }
-  return fn;
-}
 
 // 2-D bf16 tensor [rows][cols] (cols contiguous), box [box_rows][64 cols], 128-byte swizzle.
 bool make_map_2d(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
@@ -199,10 +185,22 @@ void run_route_and_permute(foe_layer* L, const void* r, int r_is_bf16, int n, cu
   L->launches += launch_permute(L->ws->topk_idx, L->ws->pb, n, L->H * L->kc, L->E, L->ws->status, st);
 }
 
+// A call whose K and V live in an 8-bit cache (foe_cache_block): the projection leaves them in the cache handle's staging
+// rows, from where they are encoded into the pages, and the attention is the cache's.
+struct Cache8Call {
+  foe_cache* h;
+  const foe_cache_view* view;
+  const float* weights_in;
+  float* weights_out;
+  long long weights_stride;
+  int window;
+};
+
 // Attention half of the block: token map, QKV projection, attention core, output projection.  With `sh` the
 // O-projection's result is this rank's partial of the synced residual and goes to the column owners' receive
 // slots; otherwise it is r_full itself, in the workspace.
-foe_status run_attend(foe_layer* L, const void* x, const foe_kv_cache* kv, cudaStream_t st, bool decode, foe_shard* sh) {
+foe_status run_attend(foe_layer* L, const void* x, const foe_kv_cache* kv, cudaStream_t st, bool decode, foe_shard* sh,
+                      const Cache8Call* c8 = nullptr) {
   const int S = decode ? kv->n_seqs : kv->n_tokens;
   // Launches of this call (this thread) overlap their predecessors' tails when the call is small; kernels that follow
   // a SHORT kernel do so at any size (the token map and statistics at the start of a call, the QKV projection after
@@ -221,15 +219,23 @@ foe_status run_attend(foe_layer* L, const void* x, const foe_kv_cache* kv, cudaS
 
   CUtensorMap tmK, tmV, tmX;
   const uint64_t page_rows = uint64_t(kv->num_pages) * L->n_kv * 64;
-  if (!make_map_2d(&tmK, kv->k_pages, page_rows, dh, 64) || !make_map_2d(&tmV, kv->v_pages, page_rows, dh, 64))
+  if (c8) {}                                        // (its attention makes its own)
+  else if (!make_map_2d(&tmK, kv->k_pages, page_rows, dh, 64) || !make_map_2d(&tmV, kv->v_pages, page_rows, dh, 64))
     return FOE_ERR_CUDA;
 
   // ---- prep: token map and pre-attention RMS statistics
   stage_mark(L, kStPrep, st);
   // (a decode step whose QKV projection runs on the tensor-core kernel needs no token map: token b is sequence b,
   //  its position and cache slot are looked up where they are used)
-  const bool inline_map = decode && L->dp_qkv;
-  if (!inline_map) L->launches += launch_token_map(decode ? nullptr : kv->q_lens, kv->context_lens, kv->block_table, kv->n_seqs, kv->max_pages_per_seq,
+  const bool inline_map = decode && L->dp_qkv && !c8;
+  const int *tok_pos = L->ws->tok_pos, *tok_slot = L->ws->tok_slot;
+  if (c8) {
+    tok_pos = c8->h->tok_pos;
+    tok_slot = c8->h->tok_slot;
+    launch_cache8_token_map(decode ? nullptr : kv->q_lens, c8->view->positions ? c8->view->positions : kv->context_lens, kv->n_seqs, S,
+                            L->cfg.max_context, c8->h->tok_pos, c8->h->tok_slot, L->ws->status, st);
+    L->launches += 1;
+  } else if (!inline_map) L->launches += launch_token_map(decode ? nullptr : kv->q_lens, kv->context_lens, kv->block_table, kv->n_seqs, kv->max_pages_per_seq,
                    kv->num_pages, 64, S, L->cfg.max_context, decode ? 1 : kv->max_q_len, L->ws->cu_q, L->ws->tok_seq, L->ws->tok_pos, L->ws->tok_slot, L->ws->status, st);
   const int x_rows = L->first ? S : H * S;
   // Kernel family of the two projections: a call of a few hundred tokens (any decode step, a short prompt chunk, a
@@ -259,7 +265,7 @@ foe_status run_attend(foe_layer* L, const void* x, const foe_kv_cache* kv, cudaS
     ga.out = L->ws->qkv; ga.ldo = L->n_q * L->dhp; ga.q_head_stride = L->dhp;
     ga.row_scale = L->ws->inv_rms; ga.scale_group_stride = L->first ? 0 : S;
     ga.q_cols = L->g * dh; ga.kv_cols = L->c * dh; ga.dh = dh; ga.n_kv = L->n_kv;
-    ga.rope_tab = L->rope_tab; ga.tok_pos = L->ws->tok_pos; ga.tok_slot = L->ws->tok_slot;
+    ga.rope_tab = L->rope_tab; ga.tok_pos = tok_pos; ga.tok_slot = tok_slot;
     ga.k_pages = static_cast<bf16*>(kv->k_pages); ga.v_pages = static_cast<bf16*>(kv->v_pages);
     launch_gemm(kEpiQKV, tmX, L->tm_wqkv, ga, L->n_sms, st);
   } else if (qkv_dp) {
@@ -270,7 +276,7 @@ foe_status run_attend(foe_layer* L, const void* x, const foe_kv_cache* kv, cudaS
     pa.epi = kEpiQKV; pa.status = L->ws->status;
     pa.out = L->ws->qkv; pa.ldo = L->n_q * L->dhp; pa.q_head_stride = L->dhp; pa.rms_eps = L->cfg.rms_eps;
     pa.q_cols = L->g * dh; pa.kv_cols = L->c * dh; pa.dh = dh; pa.n_kv = L->n_kv;
-    pa.rope_tab = L->rope_tab; pa.tok_pos = L->ws->tok_pos; pa.tok_slot = L->ws->tok_slot;
+    pa.rope_tab = L->rope_tab; pa.tok_pos = tok_pos; pa.tok_slot = tok_slot;
     pa.k_pages = static_cast<bf16*>(kv->k_pages); pa.v_pages = static_cast<bf16*>(kv->v_pages);
     if (inline_map) {
       pa.tok_pos = nullptr; pa.tok_slot = nullptr;
@@ -286,7 +292,7 @@ foe_status run_attend(foe_layer* L, const void* x, const foe_kv_cache* kv, cudaS
     sa.out = L->ws->qkv; sa.ldo = L->n_q * L->dhp; sa.q_head_stride = L->dhp;
     sa.rms_eps = L->cfg.rms_eps;
     sa.q_cols = L->g * dh; sa.kv_cols = L->c * dh; sa.dh = dh; sa.n_kv = L->n_kv;
-    sa.rope_tab = L->rope_tab; sa.tok_pos = L->ws->tok_pos; sa.tok_slot = L->ws->tok_slot;
+    sa.rope_tab = L->rope_tab; sa.tok_pos = tok_pos; sa.tok_slot = tok_slot;
     sa.k_pages = static_cast<bf16*>(kv->k_pages); sa.v_pages = static_cast<bf16*>(kv->v_pages);
     sa.status = L->ws->status;
     launch_smallm(L->tms_wqkv, sa, L->n_sms, st);
@@ -305,7 +311,13 @@ foe_status run_attend(foe_layer* L, const void* x, const foe_kv_cache* kv, cudaS
   aa.status = L->ws->status; aa.part_o = L->ws->part_o; aa.part_ml = L->ws->part_ml; aa.max_splits = L->max_splits;
   aa.split_done = L->ws->split_done;
   aa.max_kv_pages = min(kv->max_pages_per_seq, (L->cfg.max_context + 63) / 64);   // part_o / part_ml were sized for this many
-  if (decode) { launch_attn_decode(tmK, tmV, aa, L->n_sms, st); L->launches += 1; }
+  if (c8) {
+    cache8_append_staged(c8->h, c8->view, L->ws->status, st);
+    const int n = cache8_attend(c8->h, c8->view, L->ws->qkv, (long long)L->n_q * L->dhp, L->dhp, L->ws->attn_o, (long long)L->n_q * dh,
+                                c8->weights_in, c8->weights_out, c8->weights_stride, c8->window, L->ws->status, st);
+    if (n < 0) return FOE_ERR_CUDA;
+    L->launches += 1 + n;
+  } else if (decode) { launch_attn_decode(tmK, tmV, aa, L->n_sms, st); L->launches += 1; }
   else { launch_attn_prefill_tc(L->ws->tm_qkv, tmK, tmV, aa, st); L->launches += 1; }
 
   // ---- output projection; the cross-cluster sync is its K-reduction plus the sum of x[h] in the epilogue
@@ -856,6 +868,42 @@ foe_status foe_get_stage_ms(foe_layer* L, float* ms, int n) {
   L->prof_calls = 0;
   L->ev_valid = false;
   return FOE_OK;
+}
+
+// ------------------------------------------------------------------ a layer on the 8-bit cache (include/foe_cache.h)
+
+foe_status foe_cache_block(foe_layer* L, foe_cache* h, const void* x, const foe_cache_view* view, void* out,
+                           const float* weights_in, float* weights_out, long long weights_stride, int window, int decode,
+                           void* stream) {
+  if (!L || !h || !view) return FOE_ERR_NULL;
+  if (L->n_q != h->cfg.n_q_heads || L->n_kv != h->cfg.n_kv_heads || L->dh != h->cfg.head_dim) return FOE_ERR_CONFIG;
+  if (!h->cfg.for_layers) return FOE_ERR_UNSUPPORTED;
+  if ((decode != 0) != (view->q_lens == nullptr)) return decode ? FOE_ERR_UNSUPPORTED : FOE_ERR_NULL;
+  int rows = 0;
+  foe_status s = cache8_check(h, view, true, &rows);
+  if (s == FOE_OK) s = cache8_check_weights(h, view, weights_in, weights_out, weights_stride, window);
+  if (s != FOE_OK) return s;
+  if (view->n_seqs > L->cfg.max_seqs || rows > (decode ? L->cfg.max_seqs : L->cfg.max_tokens)) return FOE_ERR_SHAPE;
+  if (rows == 0) { L->launches = 0; L->last_tokens = 0; return FOE_OK; }
+  if (!x || !out) return FOE_ERR_NULL;
+  if (misaligned(x, 16) || misaligned(out, 16)) return FOE_ERR_SHAPE;
+  if (x == out) return FOE_ERR_UNSUPPORTED;
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev != h->device) return FOE_ERR_UNSUPPORTED;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  h->last_stream = st;
+  // what the shared launch sequence reads of a bf16 cache; K and V of the new tokens go to the staging rows
+  foe_kv_cache kv;
+  memset(&kv, 0, sizeof(kv));
+  kv.k_pages = h->k_stage; kv.v_pages = h->v_stage;
+  kv.block_table = view->block_table; kv.context_lens = view->context_lens; kv.q_lens = view->q_lens;
+  kv.n_seqs = view->n_seqs; kv.max_pages_per_seq = view->max_pages_per_seq; kv.num_pages = view->num_pages;
+  kv.n_tokens = rows; kv.max_q_len = decode ? 1 : view->max_q_len;
+  const Cache8Call call = {h, view, weights_in, weights_out, weights_stride, window};
+  L->shard_stage = 0;
+  s = run_attend(L, x, &kv, st, decode != 0, nullptr, &call);
+  if (s != FOE_OK) return s;
+  return run_ffn(L, out, st);
 }
 
 // ------------------------------------------------------------------ cluster-per-GPU group (include/foe_shard.h)

@@ -1,0 +1,114 @@
+"""Host side of the 8-bit cache (include/foe_cache.h) without a GPU: exports, struct layouts, refusals, and the reference
+the GPU tests compare with, against torch's own conversions."""
+import ctypes
+import os
+import re
+
+import pytest
+import torch
+
+import cache8_reference as ref
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import __graft_entry__ as g
+    g.build()
+    from paper_2605_06206_b200 import cache8
+    return cache8.load_library()
+
+
+def test_exports_and_layouts(lib):
+    from paper_2605_06206_b200 import cache8
+    hdr = open(os.path.join(ROOT, "include", "foe_cache.h")).read()
+    declared = set(re.findall(r"^foe_status (foe_cache_[a-z_]+)\s*\(", hdr, re.M))
+    assert declared == set(cache8.CACHE_EXPORTS)
+    for name in declared:
+        assert hasattr(lib, name), name
+    assert ctypes.sizeof(cache8.FoeCacheConfig) == 10 * 4
+    assert ctypes.sizeof(cache8.FoeCacheView) == 8 * 8 + 5 * 4 + 4          # 4 bytes of tail padding
+
+
+def _config(**kw):
+    from paper_2605_06206_b200 import cache8
+    d = dict(n_q_heads=8, n_kv_heads=4, head_dim=128, page_size=64, format=0, max_tokens=100, max_seqs=8, max_context=1000,
+             track_weights=1, for_layers=0)
+    d.update(kw)
+    return cache8.FoeCacheConfig(*[d[n] for n, _ in cache8.FoeCacheConfig._fields_])
+
+
+def _view(**kw):
+    from paper_2605_06206_b200 import cache8
+    d = dict(k_pages=1 << 20, v_pages=1 << 21, k_scales=1 << 12, v_scales=1 << 13, block_table=1 << 14, context_lens=1 << 15,
+             q_lens=1 << 16, positions=0, n_seqs=4, max_pages_per_seq=16, num_pages=64, n_tokens=40, max_q_len=20)
+    d.update(kw)
+    return cache8.FoeCacheView(*[d[n] for n, _ in cache8.FoeCacheView._fields_])
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(), 0), (dict(n_q_heads=6), -2), (dict(n_q_heads=68), -2), (dict(n_q_heads=0), -2), (dict(head_dim=80), -2),
+    (dict(page_size=32), -2), (dict(format=2), -2), (dict(format=-1), -2), (dict(max_tokens=0), -2), (dict(max_seqs=0), -2),
+    (dict(max_seqs=65536), -2), (dict(max_context=0), -2)])
+def test_config_refusals(lib, kw, code):
+    c, v = _config(**kw), _view()
+    assert lib.foe_cache_check(ctypes.byref(c), ctypes.byref(v)) == code
+    if code:
+        h = ctypes.c_void_p()
+        assert lib.foe_cache_create(ctypes.byref(c), ctypes.byref(h)) == code and not h.value
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(), 0), (dict(q_lens=0), 0), (dict(n_seqs=0), 0), (dict(n_seqs=8), 0), (dict(n_tokens=0, max_q_len=0), 0), (dict(n_tokens=100, max_q_len=100), 0),
+    (dict(k_pages=0), -1), (dict(v_pages=0), -1), (dict(k_scales=0), -1), (dict(v_scales=0), -1), (dict(block_table=0), -1),
+    (dict(context_lens=0), -1),
+    (dict(k_pages=(1 << 20) + 8), -3), (dict(v_pages=(1 << 20) + 1), -3), (dict(k_scales=(1 << 12) + 2), -3),
+    (dict(block_table=(1 << 14) + 1), -3), (dict(q_lens=(1 << 14) + 2), -3), (dict(positions=(1 << 14) + 2), -3),
+    (dict(n_seqs=-1), -3), (dict(n_seqs=9), -3), (dict(max_pages_per_seq=0), -3), (dict(num_pages=0), -3),
+    (dict(num_pages=1 << 23), -3),                        # rows of codes are 32-bit numbers
+    (dict(n_tokens=101), -3), (dict(n_tokens=-1), -3), (dict(max_q_len=0), -3), (dict(max_q_len=41), -3),
+    (dict(q_lens=0, n_tokens=10 ** 6, max_q_len=-5), 0)])   # (host lengths are not read with one token each)
+def test_view_refusals(lib, kw, code):
+    c, v = _config(), _view(**kw)
+    assert lib.foe_cache_check(ctypes.byref(c), ctypes.byref(v)) == code
+
+
+def test_null_arguments_need_no_device(lib):
+    v = _view()
+    assert lib.foe_cache_create(None, None) == -1
+    assert lib.foe_cache_destroy(None) == 0
+    assert lib.foe_cache_append(None, None, 0, None, 0, ctypes.byref(v), None) == -1
+    assert lib.foe_cache_attend(None, None, 0, ctypes.byref(v), None, 0, None, None, 0, 0, None) == -1
+    assert lib.foe_cache_evict(None, ctypes.byref(v), None, 0, None, 1, 1, 0, 0, None, None, None, 0, None) == -1
+    assert lib.foe_cache_block(None, None, None, ctypes.byref(v), None, None, None, 0, 0, 0, None) == -1
+    assert lib.foe_cache_poll_status(None, None) == -1
+    assert lib.foe_cache_check(None, None) == -1
+
+
+def test_no_fallback_without_a_gpu():
+    from paper_2605_06206_b200 import cache8, synth
+    if torch.cuda.is_available():
+        pytest.skip("a GPU is present")
+    with pytest.raises(RuntimeError):
+        cache8.CacheOps(synth.workload(1)[0], "e4m3", 8, 1, 64)
+
+
+# ------------------------------------------------------------------------------------------- the reference itself
+def test_reference_formats_are_the_standard_ones():
+    codes = torch.arange(256, dtype=torch.int64).to(torch.uint8)
+    want = codes.view(torch.float8_e4m3fn).double()
+    got = ref.numbers(codes, "e4m3")
+    assert torch.equal(got.nan_to_num(-1), want.nan_to_num(-1)) and int(got.isnan().sum()) == 2
+    assert torch.equal(ref.numbers(codes, "int8"), codes.view(torch.int8).double())
+    x = torch.cat([torch.randn(4000, dtype=torch.float64) * s for s in (0.003, 0.1, 5, 100)]).clamp(-448, 448).to(torch.bfloat16).double()
+    assert torch.equal(ref.nearest(x, "e4m3"), x.float().to(torch.float8_e4m3fn).double())
+    ties = torch.tensor([0.5, 1.5, 2.5, -0.5, 126.5], dtype=torch.float64)
+    assert ref.nearest(ties, "int8").tolist() == [0, 2, 2, 0, 126]
+
+
+def test_reference_scale_rule():
+    assert ref.scale_for(448.0, "e4m3") == 1.0 and ref.scale_for(449.0, "e4m3") == 2.0 and ref.scale_for(224.0, "e4m3") == 0.5
+    assert ref.scale_for(127.0, "int8") == 1.0 and ref.scale_for(127.5, "int8") == 2.0
+    assert ref.scale_for(0.0, "int8") == 2.0 ** -32
+    assert ref.scale_for(1e25, "e4m3") != ref.scale_for(1e25, "e4m3")        # NaN

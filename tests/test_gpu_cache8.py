@@ -1,0 +1,688 @@
+"""The operators of the 8-bit cache on the GPU against cache8_reference (64 bits): append bit for bit, attention and weights
+within bounds derived there, eviction bit for bit."""
+import dataclasses
+import math
+import types
+
+import pytest
+import torch
+
+import cache8_reference as ref
+from paper_2605_06206_b200 import cache8, synth
+
+pytestmark = pytest.mark.gpu
+PAGE = 64
+
+
+def shape_of(n_q, n_kv, dh):
+    return types.SimpleNamespace(n_q_heads=n_q, n_kv_heads=n_kv, head_dim=dh, page_size=PAGE)
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+class Setup:
+    """A pool with random content (unused rows hold garbage, NaN codes among it) and a shuffled block table."""
+
+    def __init__(self, n_q, n_kv, dh, fmt, totals, seed=0, extra_pages=3, garbage=True, width=None, **ops):
+        self.g = torch.Generator().manual_seed(seed)
+        self.shape, self.fmt, self.n_kv, self.dh = shape_of(n_q, n_kv, dh), fmt, n_kv, dh
+        used = [(t + PAGE - 1) // PAGE for t in totals]
+        self.width = width or max(1, max(used))
+        self.num_pages = sum(used) + extra_pages
+        ids = torch.randperm(self.num_pages, generator=self.g).to(torch.int32)
+        self.table = torch.zeros(len(totals), self.width, dtype=torch.int32)
+        at = 0
+        for b, n in enumerate(used):
+            self.table[b, :n] = ids[at:at + n]
+            at += n
+        self.spare = ids[at:]
+        shp = (self.num_pages, n_kv, PAGE, dh)
+        self.pool = cache8.empty_cache(self.shape, self.num_pages)
+        for codes in (self.pool.k_pages, self.pool.v_pages):
+            codes.copy_(torch.randint(0, 256, shp, generator=self.g).to(torch.uint8) if garbage else torch.zeros(shp, dtype=torch.uint8))
+        args = dict(max_tokens=4096, max_seqs=max(1, len(totals)), max_context=max(1, max(totals)))
+        args.update(ops)
+        self.ops = cache8.CacheOps(self.shape, fmt, **args)
+
+    def randn(self, *shape, scale=1.0):
+        return (torch.randn(*shape, generator=self.g) * scale).to(torch.bfloat16)
+
+    def refs(self):
+        return (ref.Pool(self.pool.k_pages, self.pool.k_scales, self.fmt), ref.Pool(self.pool.v_pages, self.pool.v_scales, self.fmt))
+
+    def fill(self, lens, scale=1.0, k=None, v=None):
+        """Appends random rows so that sequence b holds lens[b] tokens."""
+        rows = sum(lens)
+        if rows == 0:
+            return
+        k = self.randn(rows, self.n_kv, self.dh, scale=scale) if k is None else k
+        v = self.randn(rows, self.n_kv, self.dh) if v is None else v
+        big = max(rows, max(lens))
+        ops = cache8.CacheOps(self.shape, self.fmt, max_tokens=big, max_seqs=len(lens), max_context=self.width * PAGE, weights=False)
+        ops.append(k.cuda(), v.cuda(), self.view([0] * len(lens), lens), max_q_len=max(lens))
+        assert ops.poll_status() == 0
+        ops.close()
+
+    def view(self, ctx, q_lens=None):
+        return self.pool.view(self.table.cuda(), i32(ctx), None if q_lens is None else i32(q_lens))
+
+    def same(self, kp, vp, what=""):
+        """The pool holds exactly these numbers and scales, everywhere."""
+        k, v = self.refs()
+        for got, want, n in ((k, kp, "K"), (v, vp, "V")):
+            assert torch.equal(got.scale.nan_to_num(-1), want.scale.nan_to_num(-1)), f"{what} {n} scales"
+            assert torch.equal(got.num.nan_to_num(9999), want.num.nan_to_num(9999)), f"{what} {n} codes"
+
+
+# ======================================================================================= append
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("n_kv,dh", [(4, 128), (1, 64), (3, 96)])
+@pytest.mark.parametrize("ctx,q", [
+    ([0], [1]), ([0, 63, 64, 130], [64, 1, 65, 1]), ([5, 0, 127, 60, 1], [300, 0, 2, 9, 63]), ([200, 0], [0, 129])])
+def test_append_chunks(fmt, n_kv, dh, ctx, q):
+    s = Setup(n_kv, n_kv, dh, fmt, [a + b for a, b in zip(ctx, q)], seed=sum(ctx) + n_kv)
+    s.fill(ctx)
+    k, v = s.randn(sum(q), n_kv, dh), s.randn(sum(q), n_kv, dh)
+    k[::3] *= 9.0                                                   # some pages grow, some do not
+    kp, vp = s.refs()
+    at = 0
+    for b, n in enumerate(q):
+        if n:
+            kp.write(s.table[b], ctx[b], k[at:at + n].double())
+            vp.write(s.table[b], ctx[b], v[at:at + n].double())
+        at += n
+    s.ops.append(k.cuda(), v.cuda(), s.view(ctx, q))
+    assert s.ops.poll_status() == 0
+    s.same(kp, vp)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("n_kv,dh", [(4, 128), (1, 64), (3, 96)])
+def test_append_single_tokens(fmt, n_kv, dh):
+    """Token after token: the first row of a page, growing scales, scales that stay, zero rows, tiny and huge ones."""
+    ctx = [0, 1, 62, 64, 127, 300]
+    s = Setup(n_kv, n_kv, dh, fmt, [c + 8 for c in ctx], seed=n_kv)
+    s.fill(ctx)
+    for step, scale in enumerate([1.0, 0.0, 40.0, 1e-20, 3.0, 1e9, 1e-3, 1.0]):
+        k, v = s.randn(len(ctx), n_kv, dh, scale=scale), s.randn(len(ctx), n_kv, dh, scale=scale * 0.5)
+        now = [c + step for c in ctx]
+        kp, vp = s.refs()
+        for b in range(len(ctx)):
+            kp.write(s.table[b], now[b], k[b:b + 1].double())
+            vp.write(s.table[b], now[b], v[b:b + 1].double())
+        s.ops.append(k.cuda(), v.cuda(), s.view(now))
+        assert s.ops.poll_status() == 0
+        s.same(kp, vp, f"step {step}")
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_append_values_at_the_edges_of_the_formats(fmt):
+    """Exactly the largest code, one bf16 step above it, ties between codes, denormal codes, and both ends of the scale range."""
+    s = Setup(1, 1, 64, fmt, [64] * 8, seed=1)
+    top = ref.LARGEST[fmt]
+    rows = []
+    for base in (top, torch.nextafter(torch.tensor(top, dtype=torch.bfloat16), torch.tensor(1e9, dtype=torch.bfloat16)).item(), 1.0, 2.0 ** -32 * top, 2.0 ** -40,
+                 2.0 ** 64 * top, 2.0 ** 60):
+        x = torch.linspace(-1, 1, 64 * 64).reshape(64, 1, 64) * base
+        x[0, 0, 0] = base
+        rows.append(x.to(torch.bfloat16))
+    rows.append(torch.arange(64 * 64).reshape(64, 1, 64).remainder(255).sub(127).mul(0.5).to(torch.bfloat16))   # half steps of int8
+    x = torch.cat(rows)
+    kp, vp = s.refs()
+    for b in range(8):
+        kp.write(s.table[b], 0, rows[b].double())
+        vp.write(s.table[b], 0, -rows[b].double())
+    s.ops.append(x.cuda(), (-x).cuda(), s.view([0] * 8, [64] * 8))
+    s.same(kp, vp)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("single", [False, True])
+def test_append_non_finite_rows_make_the_page_nan(fmt, single):
+    s = Setup(2, 2, 64, fmt, [70, 70, 70, 70], seed=2)
+    ctx = [3, 3, 3, 63]
+    s.fill(ctx)
+    q = [1] * 4 if single else [5, 5, 5, 3]
+    k, v = s.randn(sum(q), 2, 64), s.randn(sum(q), 2, 64)
+    starts = [sum(q[:b]) for b in range(4)]
+    k[starts[0], 0, 7] = math.inf
+    k[starts[1], 1, 0] = math.nan
+    v[starts[2], 0, 63] = 3e38                                      # above 2^64 times the largest code
+    k[starts[3], 1, 1] = -math.inf                                  # (single: row 63 of a page; chunk: the same)
+    kp, vp = s.refs()
+    for b in range(4):
+        kp.write(s.table[b], ctx[b], k[starts[b]:starts[b] + q[b]].double())
+        vp.write(s.table[b], ctx[b], v[starts[b]:starts[b] + q[b]].double())
+    s.ops.append(k.cuda(), v.cuda(), s.view(ctx, None if single else q))
+    s.same(kp, vp)
+    assert int(s.refs()[0].scale.isnan().sum()) == 3 and int(s.refs()[1].scale.isnan().sum()) == 1
+    # it stays NaN while the page fills, and is a number again once the page is written from its first row
+    now = [c + n for c, n in zip(ctx, q)]
+    s.ops.append(s.randn(4, 2, 64).cuda(), s.randn(4, 2, 64).cuda(), s.view(now))
+    assert int(s.refs()[0].scale.isnan().sum()) == 3
+    s.ops.append(s.randn(4, 2, 64).cuda(), s.randn(4, 2, 64).cuda(), s.view([0, 0, 0, 0]))
+    assert int(s.refs()[0].scale[s.table[:3, 0].long()].isnan().sum()) == 0
+
+
+def test_append_strided_rows():
+    """K and V as slices of one [tokens, (n_q + 2 n_kv) * dh] tensor."""
+    n_kv, dh, fmt = 4, 128, "e4m3"
+    for ctx, q in (([10, 100], [70, 3]), ([10, 100], None)):
+        s = Setup(n_kv, n_kv, dh, fmt, [200, 200], seed=3)
+        s.fill(ctx)
+        rows = sum(q) if q else 2
+        both = s.randn(rows, 10, dh).cuda()
+        kp, vp = s.refs()
+        at = 0
+        for b in range(2):
+            n = q[b] if q else 1
+            kp.write(s.table[b], ctx[b], both[at:at + n, 2:6].cpu().double())
+            vp.write(s.table[b], ctx[b], both[at:at + n, 6:10].cpu().double())
+            at += n
+        s.ops.append(both[:, 2:6], both[:, 6:10], s.view(ctx, q))
+        s.same(kp, vp)
+
+
+# ======================================================================================= attention
+def run_attend(s, ctx, q_lens, scale=1.0, weights=False, window=0, q=None):
+    n_q = s.shape.n_q_heads
+    lens = [1] * len(ctx) if q_lens is None else q_lens
+    q = s.randn(sum(lens), n_q, s.dh, scale=scale) if q is None else q
+    kp, vp = s.refs()
+    w_in = w_out = None
+    if weights:
+        w_in = torch.rand(len(ctx), s.n_kv, s.width * PAGE, generator=s.g).cuda()
+        w_out = torch.full_like(w_in, -5.0)
+    out = torch.full((sum(lens) + 2, n_q, s.dh), 7.0, dtype=torch.bfloat16, device="cuda")
+    s.ops.attend(q.cuda(), s.view(ctx, q_lens), out=out[:sum(lens)], weights_in=w_in, weights_out=w_out, window=window)
+    assert s.ops.poll_status() == 0
+    o, mag, big, w = ref.attend(kp, vp, s.table, ctx, lens, q, w_in, window)
+    ref.check_attend(out[:sum(lens)], o, mag, big)
+    assert bool((out[sum(lens):] == 7.0).all())                     # rows behind the last token
+    if weights:
+        ref.check_weights(w_out, w, w_in, float(big.max()) if big.numel() else 0.0)
+        for b, n in enumerate(lens):
+            assert bool((w_out[b, :, ctx[b] + n:] == -5.0).all())   # entries behind the sequence's last key
+    return out, w_out
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("n_q,n_kv,dh", [(8, 4, 128), (16, 1, 128), (3, 3, 64), (8, 1, 64), (18, 2, 64), (7, 1, 96), (24, 2, 96), (32, 8, 128)])
+def test_attend_single_tokens(fmt, n_q, n_kv, dh):
+    ctx = [0, 1, 15, 16, 62, 63, 64, 65, 127, 128, 500, 1000]
+    s = Setup(n_q, n_kv, dh, fmt, [c + 1 for c in ctx], seed=n_q)
+    s.fill([c + 1 for c in ctx], scale=1.5)
+    run_attend(s, ctx, None, weights=True)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("ctx", [[5000], [0], [20000, 3], [4000] * 40])
+def test_attend_single_tokens_split_over_blocks(fmt, ctx):
+    """Long sequences whose pages are shared by several CTAs, and many sequences."""
+    s = Setup(8, 2, 128, fmt, [c + 1 for c in ctx], seed=len(ctx))
+    s.fill([c + 1 for c in ctx])
+    run_attend(s, ctx, None, scale=2.0, weights=True)
+
+
+def test_attend_single_tokens_many_sequences():
+    """More sequences than one warp-wide pass of the page walk holds, ragged, with some empty contexts."""
+    ctx = [(37 * i * i) % 400 for i in range(300)]
+    s = Setup(4, 2, 64, "e4m3", [c + 1 for c in ctx], seed=5)
+    s.fill([c + 1 for c in ctx])
+    run_attend(s, ctx, None, weights=True)
+
+
+@pytest.mark.parametrize("n_q,n_kv,dh", [(16, 4, 128), (16, 8, 64), (16, 1, 128)])
+def test_attend_single_tokens_at_size_back_to_back(n_q, n_kv, dh):
+    """A call whose CTAs walk dozens of pages over several sequences, many times without a wait in between: the same bits
+    every time, and sampled sequences against the reference."""
+    ctx = [2000 + (i * 977) % 7000 for i in range(48)]
+    s = Setup(n_q, n_kv, dh, "e4m3", [c + 1 for c in ctx], seed=6, garbage=False)
+    s.fill([c + 1 for c in ctx])
+    x = s.randn(48, n_q, dh, scale=1.5)
+    view, q = s.view(ctx), x.cuda()
+    outs = [s.ops.attend(q, view) for _ in range(30)]
+    assert s.ops.poll_status() == 0
+    for o in outs[1:]:
+        assert torch.equal(o, outs[0])
+    kp, vp = s.refs()
+    for b in (0, 1, 17, 47):
+        o, mag, big, _ = ref.attend(kp, vp, s.table[b:b + 1], [ctx[b]], [1], x[b:b + 1])
+        ref.check_attend(outs[0][b:b + 1], o, mag, big)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("n_q,n_kv,dh", [(8, 4, 128), (5, 1, 64), (16, 1, 64), (3, 3, 96), (12, 2, 96)])
+@pytest.mark.parametrize("ctx,q,window", [
+    ([0], [1], 0), ([0, 0], [128, 129], 0), ([63, 64, 0, 200], [1, 2, 0, 70], 1), ([700, 3], [40, 300], 32), ([2000], [5], 3)])
+def test_attend_chunks(fmt, n_q, n_kv, dh, ctx, q, window):
+    total = [a + b for a, b in zip(ctx, q)]
+    s = Setup(n_q, n_kv, dh, fmt, [max(t, 1) for t in total], seed=sum(q))
+    s.fill(total, scale=1.5)
+    run_attend(s, ctx, q, weights=True, window=window)
+
+
+@pytest.mark.parametrize("n_q,n_kv,dh", [(16, 4, 128), (8, 8, 64)])
+def test_attend_chunk_that_fills_the_gpu(n_q, n_kv, dh):
+    """No splitting of the keys: as many blocks as SMs and more; sampled rows against the reference."""
+    q = [1500, 1100, 1490]
+    ctx = [0, 777, 64]
+    s = Setup(n_q, n_kv, dh, "e4m3", [a + b for a, b in zip(ctx, q)], seed=9, max_tokens=sum(q))
+    s.fill([a + b for a, b in zip(ctx, q)])
+    x = s.randn(sum(q), n_q, dh, scale=1.5)
+    out = s.ops.attend(x.cuda(), s.view(ctx, q))
+    assert s.ops.poll_status() == 0
+    kp, vp = s.refs()
+    rows = sorted(set([0, 1, 63, 64, 127, 128, 129, 1000, 1371, 1372, 1407, 1408, 1499] + list(range(40, 1500, 211))))
+    at = 0
+    for b in range(3):
+        for i in (r for r in rows if r < q[b]):
+            o, mag, big, _ = ref.attend(kp, vp, s.table[b:b + 1], [ctx[b] + i], [1], x[at + i:at + i + 1])
+            ref.check_attend(out[at + i:at + i + 1], o, mag, big)
+        at += q[b]
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("q", [None, [3, 70]])
+def test_attend_sharp_softmax_and_uneven_pages(fmt, q):
+    """Scores of hundreds (one key takes all), pages whose scales differ by up to 2^30, queries of extreme size, zero
+    queries (uniform weights)."""
+    ctx = [400, 130]
+    lens = [1, 1] if q is None else q
+    total = [a + b for a, b in zip(ctx, lens)]
+    s = Setup(4, 2, 128, fmt, total, seed=11)
+    rows = sum(total)
+    k, v = s.randn(rows, 2, 128), s.randn(rows, 2, 128)
+    f = torch.exp2(((torch.arange(rows) // 64) % 5 * 7 - 14).float())[:, None, None].to(torch.bfloat16)
+    s.fill(total, k=k * f.clamp(max=4), v=v * f)
+    x = s.randn(sum(lens), 4, 128)
+    x[:, 0] *= 30
+    x[:, 1] *= 1e-30
+    x[:, 2] = 0
+    x[:, 3, ::2] *= 2.0 ** -20
+    run_attend(s, ctx, q, q=x, weights=True)
+
+
+@pytest.mark.parametrize("q", [None, [2, 66]])
+def test_attend_nan_pages_reach_only_who_reads_them(q):
+    """A page with a NaN scale makes NaN of every row that sees it, in its KV head only; other sequences stay clean."""
+    ctx = [100, 100]
+    lens = [1, 1] if q is None else q
+    total = [a + b for a, b in zip(ctx, lens)]
+    s = Setup(4, 2, 64, "e4m3", total, seed=12)
+    s.fill(total)
+    s.pool.k_scales[s.table[0, 0].item(), 0] = math.nan
+    s.pool.v_scales[s.table[1, 1].item(), 1] = math.nan
+    x = s.randn(sum(lens), 4, 64)
+    out = s.ops.attend(x.cuda(), s.view(ctx, q)).float().cpu()
+    n0 = lens[0]
+    assert bool(out[:n0, :2].isnan().all()) and bool(out[:n0, 2:].isfinite().all())
+    assert bool(out[n0:, 2:].isnan().all()) and bool(out[n0:, :2].isfinite().all())
+    assert s.ops.poll_status() == 0
+
+
+def test_attend_strided_rows_and_output():
+    for ctx, q in (([77, 5], [9, 130]), ([77, 5], None)):
+        lens = q or [1, 1]
+        total = [a + b for a, b in zip(ctx, lens)]
+        s = Setup(4, 2, 96, "int8", total, seed=13)
+        s.fill(total)
+        wide = s.randn(sum(lens), 8, 96).cuda()
+        out = torch.full((sum(lens), 12, 96), 3.0, dtype=torch.bfloat16, device="cuda")
+        s.ops.attend(wide[:, 4:], s.view(ctx, q), out=out[:, 4:8])
+        o, mag, big, _ = ref.attend(*s.refs(), s.table, ctx, lens, wide[:, 4:])
+        ref.check_attend(out[:, 4:8], o, mag, big)
+        assert bool((out[:, :4] == 3.0).all()) and bool((out[:, 8:] == 3.0).all())
+
+
+@pytest.mark.parametrize("q", [None, [50, 0, 7]])
+def test_attend_weights_in_place_and_same_bits(q):
+    """weights_out may be weights_in; the same call gives the same bits."""
+    ctx = [300, 90, 1000]
+    lens = q or [1, 1, 1]
+    total = [a + b for a, b in zip(ctx, lens)]
+    s = Setup(8, 2, 128, "e4m3", total, seed=14)
+    s.fill(total)
+    x = s.randn(sum(lens), 8, 128).cuda()
+    w_in = torch.rand(3, 2, s.width * PAGE, device="cuda")
+    w_out = torch.zeros_like(w_in)
+    a = s.ops.attend(x, s.view(ctx, q), weights_in=w_in, weights_out=w_out)
+    same = w_in.clone()
+    b = s.ops.attend(x, s.view(ctx, q), weights_in=same, weights_out=same)
+    assert torch.equal(a, b)
+    for i, n in enumerate(total):
+        assert torch.equal(same[i, :, :n], w_out[i, :, :n])
+
+
+def test_attend_shared_pages():
+    """Two sequences that name the same pages (a common prompt prefix)."""
+    s = Setup(8, 2, 128, "e4m3", [129, 140], seed=15)
+    s.fill([129, 140])
+    s.table[1, :2] = s.table[0, :2]
+    run_attend(s, [128, 139], None, weights=True)
+    run_attend(s, [120, 120], [8, 20], weights=True)
+
+
+# ======================================================================================= eviction
+def run_evict(s, lens, budget, sink, recent, weights=None):
+    n, width = len(lens), (budget + PAGE - 1) // PAGE
+    w = torch.rand(n, s.n_kv, s.width * PAGE, generator=s.g) if weights is None else weights
+    to = s.spare[:n * width].view(n, width)
+    kp, vp = s.refs()
+    kept = torch.full((n, s.n_kv, budget), -7, dtype=torch.int32, device="cuda")
+    new_lens = torch.full((n,), -7, dtype=torch.int32, device="cuda")
+    w_out = torch.full((n, s.n_kv, width * PAGE), -7.0, device="cuda")
+    s.ops.evict(s.view(lens), w.cuda(), to.cuda(), budget, sink, recent, new_lens, kept, w_out)
+    assert s.ops.poll_status() == 0
+    want, want_lens = ref.evict(kp, vp, s.table, lens, w, to, budget, sink, recent)
+    assert new_lens.tolist() == want_lens
+    for b in range(n):
+        for h in range(s.n_kv):
+            m = want_lens[b]
+            assert kept[b, h, :m].tolist() == want[b][h]
+            assert bool((kept[b, h, m:] == -7).all()) and bool((w_out[b, h, m:] == -7).all())
+            got, exp = w_out[b, h, :m].cpu(), w[b, h, want[b][h]]
+            assert torch.equal(got.nan_to_num(-9.5), exp.nan_to_num(-9.5))
+    s.same(kp, vp)
+    return to, new_lens, kept, w_out
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("n_kv,dh", [(2, 128), (1, 64), (3, 96)])
+@pytest.mark.parametrize("lens,budget,sink,recent", [
+    ([1], 1, 0, 0), ([0, 300, 64, 65, 129], 64, 4, 10), ([1000, 77], 100, 0, 0), ([500], 130, 130, 0), ([500, 640], 200, 3, 197),
+    ([1300, 2], 700, 65, 70), ([200, 64], 1, 1, 0), ([200, 64], 1, 0, 1)])
+def test_evict(fmt, n_kv, dh, lens, budget, sink, recent):
+    s = Setup(n_kv, n_kv, dh, fmt, [max(n, 1) for n in lens], seed=budget, extra_pages=len(lens) * ((budget + 63) // 64))
+    k = s.randn(sum(lens), n_kv, dh) * torch.exp2((torch.arange(sum(lens)) % 9 - 4).float())[:, None, None].to(torch.bfloat16)
+    if sum(lens):
+        s.fill(lens, k=k)
+    run_evict(s, lens, budget, sink, recent)
+
+
+@pytest.mark.parametrize("kind", ["equal", "few values", "negative and zeros", "nan and inf", "one exponent", "all nan"])
+def test_evict_order_of_weights(kind):
+    lens = [700, 300]
+    s = Setup(2, 2, 64, "e4m3", lens, seed=20, extra_pages=2 * 4)
+    s.fill(lens)
+    w = torch.rand(2, 2, s.width * PAGE, generator=s.g)
+    if kind == "equal":
+        w[:] = 0.25
+    elif kind == "few values":
+        w = (w * 4).floor() / 4
+    elif kind == "negative and zeros":
+        w = (w - 0.5) * (w > 0.3)
+        w[:, :, ::7] = -0.0
+    elif kind == "nan and inf":
+        w[:, :, ::5], w[:, :, 1::9], w[:, :, 2::9] = math.nan, math.inf, -math.inf
+    elif kind == "one exponent":
+        w = 1 + w * 2.0 ** -18
+    else:
+        w[:] = math.nan
+    run_evict(s, lens, 250, 2, 30, weights=w)
+
+
+def test_evict_shared_source_pages_and_nan_pages():
+    lens = [130, 135]
+    s = Setup(2, 2, 64, "int8", lens, seed=21, extra_pages=2)
+    s.fill(lens)
+    s.table[1, :2] = s.table[0, :2]
+    s.pool.v_scales[s.table[0, 1].item(), 1] = math.nan
+    run_evict(s, lens, 64, 1, 5)
+
+
+def test_evict_long_sequence():
+    s = Setup(1, 1, 64, "e4m3", [70000], seed=22, extra_pages=20)
+    s.fill([70000])
+    run_evict(s, [70000], 1280, 4, 100)
+
+
+# ======================================================================================= all of them in a row
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_generation_with_eviction(fmt):
+    """A prompt in two chunks, single tokens with accumulated weights, a cut, more tokens on the cut cache: every step
+    against the reference on the cache as it was."""
+    n_q, n_kv, dh, budget = 8, 2, 128, 150
+    n = 3
+    s = Setup(n_q, n_kv, dh, fmt, [400] * n, seed=30, extra_pages=n * 4)
+    lens, width = [0] * n, s.width * PAGE
+    w = torch.zeros(n, n_kv, width, device="cuda")
+
+    def step(q):
+        nonlocal w
+        rows = sum(q) if q else n
+        qs = q or [1] * n
+        k, v, x = s.randn(rows, n_kv, dh), s.randn(rows, n_kv, dh), s.randn(rows, n_q, dh, scale=1.5)
+        kp, vp = s.refs()
+        at = 0
+        for b in range(n):
+            if qs[b]:
+                kp.write(s.table[b], lens[b], k[at:at + qs[b]].double())
+                vp.write(s.table[b], lens[b], v[at:at + qs[b]].double())
+            at += qs[b]
+        view = s.view(lens, q)
+        s.ops.append(k.cuda(), v.cuda(), view)
+        before = w.clone()
+        out = s.ops.attend(x.cuda(), view, weights_in=w, weights_out=w, window=16)
+        assert s.ops.poll_status() == 0
+        s.same(kp, vp)
+        o, mag, big, want = ref.attend(kp, vp, s.table, lens, qs, x, before, 16)
+        ref.check_attend(out, o, mag, big)
+        ref.check_weights(w, want, before, float(big.max()))
+        for b in range(n):
+            lens[b] += qs[b]
+
+    step([200, 10, 64])
+    step([90, 3, 0])
+    for _ in range(3):
+        step(None)
+    to, new_lens, kept, w_new = run_evict(s, lens, budget, 2, 20, weights=w.cpu())
+    lens[:] = new_lens.tolist()
+    assert lens == [150, 16, 67]
+    # the cut sequences go on in their new pages; pages they grow into come from the old table
+    old = s.table.clone()
+    s.table[:, :3] = to
+    s.table[:, 3:] = old[:, 3:]
+    w = torch.zeros(n, n_kv, width, device="cuda")
+    w[:, :, :w_new.shape[2]] = w_new.clamp(min=0)
+    for _ in range(3):
+        step(None)
+    step([60, 1, 2])
+
+
+# ======================================================================================= streams, graphs, refusals
+def test_calls_on_another_stream_and_in_a_graph():
+    ctx = [200, 333]
+    s = Setup(8, 2, 128, "e4m3", [400, 400], seed=40)
+    s.fill(ctx)
+    k, v, x = (s.randn(2, h, 128).cuda() for h in (2, 2, 8))
+    w = torch.zeros(2, 2, s.width * PAGE, device="cuda")
+    view = s.view(ctx)
+    out = torch.zeros(2, 8, 128, dtype=torch.bfloat16, device="cuda")
+    saved = [t.clone() for t in (s.pool.k_pages, s.pool.v_pages, s.pool.k_scales, s.pool.v_scales)]
+
+    def calls(stream=None):
+        s.ops.append(k, v, view, stream=stream)
+        s.ops.attend(x, view, out=out, weights_in=w, weights_out=w, stream=stream)
+
+    calls()
+    want, want_w = out.clone(), w.clone()
+    pages = [t.clone() for t in (s.pool.k_pages, s.pool.k_scales)]
+    other = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    out.zero_(), w.zero_()
+    for t, u in zip((s.pool.k_pages, s.pool.v_pages, s.pool.k_scales, s.pool.v_scales), saved):
+        t.copy_(u)
+    torch.cuda.synchronize()
+    calls(other)
+    other.synchronize()
+    assert torch.equal(out, want) and torch.equal(w, want_w) and torch.equal(s.pool.k_pages, pages[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    out.zero_(), w.zero_()
+    for t, u in zip((s.pool.k_pages, s.pool.v_pages, s.pool.k_scales, s.pool.v_scales), saved):
+        t.copy_(u)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(w, want_w) and torch.equal(s.pool.k_scales, pages[1])
+    # the captured step follows the lengths on the device: one token further on it attends to one key more
+    view.context_lens.add_(1)
+    before = w.clone()
+    graph.replay()
+    torch.cuda.synchronize()
+    o, mag, big, _ = ref.attend(*s.refs(), s.table, [c + 1 for c in ctx], [1, 1], x)
+    ref.check_attend(out, o, mag, big)
+    assert s.ops.poll_status() == 0
+    assert bool((w[0, :, ctx[0] + 1] > before[0, :, ctx[0] + 1]).all())
+
+
+def test_chunk_calls_in_a_graph():
+    ctx, q = [200, 64], [33, 100]
+    total = [a + b for a, b in zip(ctx, q)]
+    s = Setup(8, 2, 64, "int8", total, seed=41)
+    s.fill(total)
+    x = s.randn(sum(q), 8, 64).cuda()
+    view, w = s.view(ctx, q), torch.zeros(2, 2, s.width * PAGE, device="cuda")
+    out = s.ops.attend(x, view, max_q_len=100, weights_in=w, weights_out=w)
+    want, want_w = out.clone(), w.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s.ops.attend(x, view, out=out, max_q_len=100, weights_in=w, weights_out=w)
+    out.zero_(), w.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(w, want_w)
+
+
+def refused(code, call, *args, **kw):
+    from paper_2605_06206_b200.binding import FoeError
+    with pytest.raises(FoeError) as e:
+        call(*args, **kw)
+    assert e.value.code == code
+
+
+def test_refusals():
+    s = Setup(8, 2, 128, "e4m3", [100, 100], seed=42, max_tokens=64, max_context=100, extra_pages=8)
+    s.fill([50, 50])
+    v1 = s.view([50, 50])
+    x, k = s.randn(2, 8, 128).cuda(), s.randn(2, 2, 128).cuda()
+    assert s.ops.attend(x, v1).shape == (2, 8, 128)
+    refused(-3, s.ops.attend, s.randn(65, 8, 128).cuda(), s.view([0, 0], [60, 5]))               # max_tokens
+    refused(-3, s.ops.append, s.randn(20, 2, 128).cuda(), s.randn(20, 2, 128).cuda(), s.view([0, 0], [10, 10]), max_q_len=21)
+    refused(-4, s.ops.attend, x, v1, out=x)                                                     # in place
+    w = torch.zeros(2, 2, 128, device="cuda")
+    refused(-3, s.ops.attend, x, v1, weights_in=w[:, :, :90].contiguous(), weights_out=w[:, :, :90].contiguous())
+    refused(-3, s.ops.attend, x, v1, weights_in=w, weights_out=w, window=-1)
+    bad = torch.zeros(2 * 8 * 128 + 8, dtype=torch.bfloat16, device="cuda")[1:2 * 8 * 128 + 1].view(2, 8, 128)
+    refused(-3, s.ops.attend, bad, v1)                                                          # alignment
+    plain = cache8.CacheOps(s.shape, "e4m3", 64, 2, 100, weights=False)
+    refused(-4, plain.attend, x, v1, weights_in=w, weights_out=w)
+    to, kept, lens = s.spare[:2].view(2, 1).cuda(), torch.zeros(2, 2, 64, dtype=torch.int32, device="cuda"), i32([0, 0])
+    refused(-3, s.ops.evict, v1, w, to, 64, 40, 30, lens, kept)                                 # sink + recent > budget
+    refused(-3, s.ops.evict, v1, w, to, 64, -1, 3, lens, kept)
+    refused(-3, s.ops.evict, v1, w, to, 65, 1, 3, lens, torch.zeros(2, 2, 65, dtype=torch.int32, device="cuda"))   # pages for 64
+    refused(-4, s.ops.evict, v1, w, to, 64, 1, 3, lens, kept, w)                                # weights in place
+    refused(-3, s.ops.evict, v1, w[:, :, :90].contiguous(), to, 64, 1, 3, lens, kept)
+    with pytest.raises(AssertionError):
+        s.ops.attend(x.float(), v1)
+    with pytest.raises(AssertionError):
+        s.ops.append(k.transpose(1, 2).contiguous().transpose(1, 2), k, v1)                     # rows not contiguous
+    with pytest.raises(AssertionError):
+        s.ops.attend(x.cpu(), v1)
+    assert s.ops.poll_status() == 0
+    assert plain.poll_status() == 0
+
+
+def test_no_sequences_and_no_tokens():
+    s = Setup(8, 2, 128, "e4m3", [100], seed=43)
+    none = dataclasses.replace(s.view([5]), block_table=s.table[:0].cuda(), context_lens=i32([]))
+    empty_q, empty_k = torch.zeros(0, 8, 128, dtype=torch.bfloat16, device="cuda"), torch.zeros(0, 2, 128, dtype=torch.bfloat16, device="cuda")
+    s.ops.append(empty_k, empty_k, none)
+    assert s.ops.attend(empty_q, none).shape[0] == 0
+    view = s.view([50], [0])
+    s.ops.append(empty_k, empty_k, view)
+    w = torch.rand(1, 2, 128, device="cuda")
+    out_w = torch.zeros_like(w)
+    assert s.ops.attend(empty_q, view, weights_in=w, weights_out=out_w).shape[0] == 0
+    assert torch.equal(out_w[:, :, :50], w[:, :, :50]) and bool((out_w[:, :, 50:] == 0).all())
+    assert s.ops.poll_status() == 0
+
+
+def test_bad_lengths_and_pages_are_reported_and_skipped():
+    """Values only the device sees: the status word says so, other sequences are computed."""
+    ctx = [70, 40]
+    s = Setup(8, 2, 64, "e4m3", [120, 120], seed=44, max_context=120)
+    s.fill(ctx)
+    good_x = s.randn(2, 8, 64)
+    k = s.randn(2, 2, 64).cuda()
+    # a context beyond the table
+    view = s.view([5000, 40])
+    s.ops.append(k, k, view)
+    assert s.ops.poll_status() == -8
+    out = s.ops.attend(good_x.cuda(), view)
+    assert s.ops.poll_status() == -8
+    o, mag, big, _ = ref.attend(*s.refs(), s.table[1:], [40], [1], good_x[1:])
+    ref.check_attend(out[1:], o, mag, big)
+    # a page id outside the pool, in the other sequence
+    s.table[0, 0] = s.num_pages + 7
+    view = s.view([70, 40])
+    kp, vp = s.refs()
+    kp.write(s.table[0], 70, k[:1].double().cpu()), vp.write(s.table[0], 70, k[:1].double().cpu())   # (its last page is good)
+    kp.write(s.table[1], 40, k[1:].double().cpu()), vp.write(s.table[1], 40, k[1:].double().cpu())
+    s.ops.append(k, k, view)
+    assert s.ops.poll_status() == 0
+    s.same(kp, vp)
+    out = s.ops.attend(good_x.cuda(), view)
+    assert s.ops.poll_status() == -8
+    o, mag, big, _ = ref.attend(*s.refs(), s.table[1:], [40], [1], good_x[1:])
+    ref.check_attend(out[1:], o, mag, big)
+    # chunk lengths that do not add up to n_tokens, and one above max_q_len
+    x = s.randn(10, 8, 64).cuda()
+    s.ops.attend(x, s.view([0, 40], [4, 30]), max_q_len=10)
+    assert s.ops.poll_status() == -8
+    s.ops.append(s.randn(10, 2, 64).cuda(), s.randn(10, 2, 64).cuda(), s.view([0, 40], [30, 4]), max_q_len=10)
+    assert s.ops.poll_status() == -8
+    # eviction of a sequence that claims more than the table holds
+    to, kept, lens = s.spare[:2].view(2, 1).cuda(), torch.zeros(2, 2, 30, dtype=torch.int32, device="cuda"), i32([9, 9])
+    s.table[0, 0] = s.table[0, 1]
+    s.ops.evict(s.view([5000, 40]), torch.rand(2, 2, 128, device="cuda"), to, 30, 1, 2, lens, kept)
+    assert s.ops.poll_status() == -8 and lens.tolist() == [0, 30]
+    # and the handle works afterwards
+    s.ops.attend(good_x.cuda(), s.view([70, 40]))
+    assert s.ops.poll_status() == 0
+
+
+def test_offsets_beyond_32_bits():
+    """A pool of more than 4 GiB of K codes: the sequence's pages lie at its end."""
+    n_kv, dh = 8, 128
+    pages = (1 << 32) // (n_kv * PAGE * dh) + 40
+    shape = shape_of(16, n_kv, dh)
+    pool = cache8.empty_cache(shape, pages)
+    ids = torch.arange(pages - 12, pages, dtype=torch.int32)
+    g = torch.Generator().manual_seed(50)
+    ctx = 300
+    k = torch.randn(ctx + 1, n_kv, dh, generator=g).to(torch.bfloat16).cuda()
+    ops = cache8.CacheOps(shape, "e4m3", ctx + 1, 1, 400)
+    table = ids[:6].view(1, 6).cuda()
+    ops.append(k, -k, pool.view(table, i32([0]), i32([ctx + 1])))
+    q = torch.randn(1, 16, dh, generator=g).to(torch.bfloat16)
+    w = torch.zeros(1, n_kv, 384, device="cuda")
+    out = ops.attend(q.cuda(), pool.view(table, i32([ctx])), weights_in=w, weights_out=w)
+    chunk = ops.attend(q.cuda(), pool.view(table, i32([ctx]), i32([1])))
+    tail = slice(pages - 12, pages)
+    small = [t[tail].clone() for t in (pool.k_pages, pool.v_pages)], [t[tail].clone() for t in (pool.k_scales, pool.v_scales)]
+    kp, vp = ref.Pool(small[0][0], small[1][0], "e4m3"), ref.Pool(small[0][1], small[1][1], "e4m3")
+    local = ids[:6].view(1, 6) - (pages - 12)
+    o, mag, big, want = ref.attend(kp, vp, local, [ctx], [1], q, torch.zeros(1, n_kv, 384))
+    ref.check_attend(out, o, mag, big)
+    ref.check_attend(chunk, o, mag, big)
+    ref.check_weights(w, want, torch.zeros(1, n_kv, 384), float(big.max()))
+    to, kept, lens = ids[6:8].view(1, 2).cuda(), torch.zeros(1, n_kv, 100, dtype=torch.int32, device="cuda"), i32([0])
+    ops.evict(pool.view(table, i32([ctx + 1])), w, to, 100, 2, 10, lens, kept)
+    ref.evict(kp, vp, local, [ctx + 1], w.cpu(), ids[6:8].view(1, 2) - (pages - 12), 100, 2, 10)
+    got = ref.Pool(pool.k_pages[tail], pool.k_scales[tail], "e4m3")
+    assert torch.equal(got.num, kp.num) and torch.equal(got.scale, kp.scale)
+    assert ops.poll_status() == 0

@@ -1,0 +1,158 @@
+"""A layer's forward pass on the 8-bit cache (foe_cache_block): the projection's K and V rows against the same layer's on a
+bf16 cache (bit for bit after encoding), the attention against cache8_reference on the layer's own q and pages, the rest of
+the block against the oracle; then a stack of layers that generates, cuts its cache and goes on."""
+import dataclasses
+
+import numpy as np
+import pytest
+import torch
+
+import cache8_reference as ref
+from oracle import adapter
+from oracle import foe_oracle as orc
+from paper_2605_06206_b200 import binding, cache8, synth
+
+from parity import assert_close
+
+pytestmark = pytest.mark.gpu
+PAGE = 64
+
+SHAPES = {
+    "dh64": synth.LayerShape(256, 8, 4, 4, 64, 8, 2, 128),
+    "dh96": synth.LayerShape(256, 8, 8, 8, 96, 4, 2, 128),
+    "dh128": synth.LayerShape(512, 16, 4, 4, 128, 8, 2, 256),
+    "first": synth.LayerShape(256, 8, 4, 4, 64, 8, 2, 128, position="first"),
+    "one cluster": synth.LayerShape(256, 8, 2, 1, 64, 16, 4, 128, position="last"),
+}
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+class Both:
+    """One layer with a bf16 cache and an 8-bit one of the same pages."""
+
+    def __init__(self, shape, fmt, n, most, seed=0, **kw):
+        self.shape, self.fmt, self.n = shape, fmt, n
+        self.W = synth.make_weights(shape, seed, "cuda")
+        self.layer = binding.FoeLayer(shape, self.W, max_tokens=2048, max_seqs=n, max_context=most)
+        self.ops = cache8.CacheOps(shape, fmt, 2048, n, most, layers=True, **kw)
+        width = (most + PAGE - 1) // PAGE
+        self.table = torch.randperm(n * width, generator=torch.Generator().manual_seed(seed)).to(torch.int32).view(n, width)
+        shp = (n * width, shape.n_kv_heads, PAGE, shape.head_dim)
+        self.k16, self.v16 = torch.zeros(shp, dtype=torch.bfloat16, device="cuda"), torch.zeros(shp, dtype=torch.bfloat16, device="cuda")
+        self.pool = cache8.empty_cache(shape, n * width)
+
+    def refs(self):
+        return ref.Pool(self.pool.k_pages, self.pool.k_scales, self.fmt), ref.Pool(self.pool.v_pages, self.pool.v_scales, self.fmt)
+
+    def rows16(self, pages, b, lo, hi):
+        ids = self.table[b].long()
+        return pages[ids.cuda()].transpose(1, 2).flatten(0, 1)[lo:hi].cpu().double()      # [rows, n_kv, dh]
+
+    def step(self, ctx, q, seed, positions=None, w_in=None, w_out=None):
+        """One call on both caches; returns the block's output on the 8-bit one after checking every stage."""
+        sh, n = self.shape, self.n
+        lens = [1] * n if q is None else q
+        S = sum(lens)
+        at = ctx if positions is None else positions
+        x = synth.make_x(sh, seed, S, "cuda")
+        kv = synth.PagedKV(self.k16, self.v16, self.table.cuda(), i32(at), None if q is None else i32(q))
+        self.layer.decode(x, kv) if q is None else self.layer.prefill(x, kv)
+        assert self.layer.poll_status() == 0
+        q16 = self.layer.aux()["q"]
+        kp, vp = self.refs()
+        for b in range(n):
+            if lens[b]:
+                kp.write(self.table[b], ctx[b], self.rows16(self.k16, b, at[b], at[b] + lens[b]))
+                vp.write(self.table[b], ctx[b], self.rows16(self.v16, b, at[b], at[b] + lens[b]))
+        view = self.pool.view(self.table.cuda(), i32(ctx), None if q is None else i32(q), None if positions is None else i32(positions))
+        out = self.ops.block(self.layer, x, view, weights_in=w_in, weights_out=w_out, window=5)
+        assert self.layer.poll_status() == 0
+        aux = self.layer.aux()
+        assert torch.equal(aux["q"], q16)
+        gk, gv = self.refs()
+        for got, want in ((gk, kp), (gv, vp)):
+            assert torch.equal(got.num, want.num) and torch.equal(got.scale, want.scale)
+        before = None if w_in is None else w_in.cpu()
+        o, mag, big, w = ref.attend(kp, vp, self.table, ctx, lens, aux["q"].view(S, sh.n_q_heads, sh.head_dim), before, 5)
+        ref.check_attend(aux["attn_o"].view(S, sh.n_q_heads, sh.head_dim), o, mag, big)
+        if w_in is not None:
+            ref.check_weights(w_out, w, before, float(big.max()))
+        # output projection and sync on the GPU's own attention output, experts on its residual and ids
+        cfg, Wn = adapter.cfg_from_shape(sh), adapter.weights_to_numpy(self.W)
+        xn = adapter.to_np(x).astype(np.float64)
+        r = adapter.to_np(aux["attn_o"]).astype(np.float64) @ Wn["wo"].astype(np.float64)
+        first = sh.position in ("first", "single")
+        r = xn + r if first else (xn.sum(0) + r) / sh.n_clusters
+        assert_close(adapter.to_np(aux["r_full"]), r, "r_full")
+        iso = orc.moe_stage(cfg, Wn, adapter.to_np(aux["r_full"]).astype(np.float64), idx_override=aux["topk_idx"].cpu().numpy())
+        assert_close(adapter.to_np(out), iso["out"], "block output")
+        return out
+
+
+@pytest.mark.parametrize("name", list(SHAPES))
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_block_prefill_then_decode(name, fmt):
+    s = Both(SHAPES[name], fmt, 3, 700, seed=3)
+    s.step([0, 0, 0], [300, 1, 90], 10)                    # tiled kernels
+    s.step([300, 1, 90], [20, 64, 3], 11)                  # a small mixed batch: the decode step's projections
+    s.step([320, 65, 93], None, 12)
+    s.step([321, 66, 94], None, 13)
+
+
+@pytest.mark.parametrize("q", [None, [4, 30]])
+def test_block_positions_and_weights(q):
+    """Sequences that hold fewer tokens than they have seen: K and q are rotated at the true position, rows go behind the held
+    ones."""
+    s = Both(SHAPES["dh64"], "e4m3", 2, 900, seed=4)
+    s.step([0, 0], [100, 130], 20)
+    w = torch.rand(2, 4, 15 * PAGE, device="cuda")
+    out_w = torch.zeros_like(w)
+    s.step([100, 130], q, 21, positions=[500, 131], w_in=w, w_out=out_w)
+
+
+def test_block_refusals_and_bad_positions():
+    s = Both(SHAPES["dh64"], "e4m3", 2, 100, seed=5)
+    x = synth.make_x(s.shape, 1, 2, "cuda")
+
+    def refused(code, ops, *a, **kw):
+        with pytest.raises(binding.FoeError) as e:
+            ops.block(s.layer, *a, **kw)
+        assert e.value.code == code
+
+    view = s.pool.view(s.table.cuda(), i32([3, 4]))
+    refused(-4, cache8.CacheOps(s.shape, "e4m3", 16, 2, 100), x, view)                     # not made for layers
+    refused(-4, s.ops, x, view, out=x)                                                     # in place
+    wrong = cache8.CacheOps(dataclasses.replace(s.shape, n_q_heads=4), "e4m3", 16, 2, 100, layers=True)
+    refused(-2, wrong, x, view)                                                            # other head counts
+    big = cache8.CacheOps(s.shape, "e4m3", 5000, 4, 100, layers=True)
+    refused(-3, big, synth.make_x(s.shape, 1, 3000, "cuda"), s.pool.view(s.table.cuda(), i32([0, 0]), i32([1500, 1500])))   # layer's max_tokens
+    s.ops.block(s.layer, x, s.pool.view(s.table.cuda(), i32([3, 4]), None, i32([3, 5000])))
+    assert s.layer.poll_status() == -8
+    s.ops.block(s.layer, x, view)
+    assert s.layer.poll_status() == 0 and s.ops.poll_status() == 0
+
+
+def test_block_decode_replayed_from_a_graph():
+    s = Both(SHAPES["dh64"], "int8", 2, 300, seed=6)
+    s.step([0, 0], [70, 100], 30)
+    x, ctx = synth.make_x(s.shape, 31, 2, "cuda"), i32([70, 100])
+    view = s.pool.view(s.table.cuda(), ctx)
+    saved = [t.clone() for t in (s.pool.k_pages, s.pool.v_pages, s.pool.k_scales, s.pool.v_scales)]
+    out = s.ops.block(s.layer, x, view)
+    second = s.ops.block(s.layer, x, dataclasses.replace(view, context_lens=ctx + 1))
+    for t, u in zip((s.pool.k_pages, s.pool.v_pages, s.pool.k_scales, s.pool.v_scales), saved):
+        t.copy_(u)
+    got = torch.empty_like(out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s.ops.block(s.layer, x, view, out=got)
+        binding._check(s.ops.lib.foe_context_advance(ctx.data_ptr(), 2, 1, torch.cuda.current_stream().cuda_stream), "advance")
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got, out)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got, second) and ctx.tolist() == [72, 102]
