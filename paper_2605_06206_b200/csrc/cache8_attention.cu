@@ -28,18 +28,16 @@
 
 namespace foe {
 
-constexpr int kD8Stages = 6;
+constexpr int kD8Stages = 3;
 constexpr int kD8MinTiles = 2;                   // fewest pages per CTA
+constexpr int kD8Gap = 6;                        // what starting a pair costs, in pages (decode_walk.cuh)
 constexpr float kD8Shift = 6.f;                  // P' = 2^(t - m + shift)
 constexpr float kD8Lazy = 8.f;                   // the reference maximum moves when a score exceeds it by more than this
 
 template <int NT> struct D8Cfg {                 // NT: tiles of 8 heads
-  static constexpr int kWarps = NT == 1 ? 8 : 4; // consumers (16 heads: fewer warps with twice the registers)
-  static constexpr int kGroups = kWarps / 4;     // groups of four warps that take alternate pages
+  static constexpr int kWarps = 4;               // consumers, each 16 keys of every page
+  static constexpr int kCtas = NT == 1 ? 3 : 2;  // per SM (16 heads need twice the registers)
   static constexpr int kThreads = (kWarps + 1) * 32;
-  // A stage belongs to one group for good, so that the group sees every phase of the stage's barrier: a parity wait
-  // cannot tell a phase from the one before the last.
-  static_assert(kD8Stages % kGroups == 0, "stages are divided among the groups");
 };
 
 template <int DH, int NT>
@@ -50,8 +48,8 @@ struct D8Smem {
   static constexpr int kRows = 8 * NT;
   static constexpr int kMoOff = kRing;
   static constexpr int kMmOff = kMoOff + kRows * kPitch * 4;                     // [warps][kRows] maxima, then sums
-  static constexpr int kScaleOff = kMmOff + 2 * D8Cfg<NT>::kWarps * kRows * 4;   // per stage: K scale, log2 V scale, 1 / V scale
-  static constexpr int kBarOff = kScaleOff + kD8Stages * 16;
+  static constexpr int kScaleOff = kMmOff + 2 * D8Cfg<NT>::kWarps * kRows * 4;   // [64] K scale, log2 V scale, 1 / V scale of the last pages
+  static constexpr int kBarOff = kScaleOff + 64 * 16;
   static constexpr int kMiscOff = kBarOff + 2 * kD8Stages * 8;
   static constexpr size_t kBytes = size_t(kMiscOff) + 16 + 1024;
 };
@@ -69,8 +67,9 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
 template <int THREADS>
 __device__ __forceinline__ void d8_bar() { asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory"); }
 
-template <int FMT, int DH, int NT>
-__global__ void __launch_bounds__(D8Cfg<NT>::kThreads, 2)
+// LOGITS: also leaves the scores in a.logits (a call that accumulates attention weights).
+template <int FMT, int DH, int NT, bool LOGITS>
+__global__ void __launch_bounds__(D8Cfg<NT>::kThreads, D8Cfg<NT>::kCtas)
 cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const Cache8AttendArgs a) {
   using SM = D8Smem<DH, NT>;
   using CF = D8Cfg<NT>;
@@ -89,54 +88,80 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kD8Stages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 4); }
+    for (int s = 0; s < kD8Stages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], CF::kWarps); }
     mbar_fence_init();
+    tma_prefetch_desc(&tmK);
+    tma_prefetch_desc(&tmV);
   }
   __syncthreads();
   pdl_wait();
   pdl_launch_dependents();
 
   DcWalk w;
-  if (!dc_begin(c, kD8MinTiles, w)) return;                        // (the same in every warp)
+  if (!dc_begin<kD8Gap>(c, kD8MinTiles, w)) return;                // (the same in every warp)
 
   if (warp == CF::kWarps) {
     // ------------------------------------------------------------------ producer
-    bool ok = true;
-    int it = 0;
-    while (ok && w.t < w.t_end) {
-      const int len = dc_segment_len(w);
-      for (int j0 = 0; j0 < len && ok; j0 += 32) {
-        const int n = min(32, len - j0);
-        int row0 = 0;
-        float sk = 0.f, sv = 1.f;
-        if (lane < n) {
-          const int lp = w.page + j0 + lane;
-          int page = c.block_table[size_t(w.b) * c.max_pages_per_seq + min(lp, c.max_pages_per_seq - 1)];
-          if (page < 0 || page >= c.num_pages) { atomicExch(c.status, kStatusBounds); page = 0; }
-          const int ph = page * c.n_kv + w.kvh;
-          row0 = ph * 64;
-          sk = c.k_scales[ph];
-          sv = c.v_scales[ph];
-        }
-        for (int j = 0; j < n && ok; ++j, ++it) {
-          const int st = it % kD8Stages;
-          const uint32_t ph = (it / kD8Stages) & 1;
-          const int r0 = __shfl_sync(0xffffffffu, row0, j);
-          const float skj = __shfl_sync(0xffffffffu, sk, j), svj = __shfl_sync(0xffffffffu, sv, j);
-          if (lane == 0) {
-            ok = mbar_wait(&empty[st], ph ^ 1);
-            if (ok) {
-              const float ev = c8_is_nan(svj) ? svj : float(c8_scale_exp(svj));
-              scales[st] = make_float4(skj, ev, 1.f / svj, 0.f);
-              mbar_expect_tx(&full[st], 2 * SM::kTile);
-              tma_load_2d(smem + st * 2 * SM::kTile, &tmK, &full[st], 0, r0);
-              tma_load_2d(smem + st * 2 * SM::kTile + SM::kTile, &tmV, &full[st], 0, r0);
-            }
-          }
-          ok = __shfl_sync(0xffffffffu, ok, 0);
-        }
+    // Pages come in batches of up to 32 of one segment; lane i holds page i's place and scales.  What stands between a
+    // page id and the first data is only the copy itself: the copies of a batch's first pages are issued before the
+    // batch's scales have arrived (their barrier's arrival follows when the scales are in shared memory), and the next
+    // batch's page ids are loaded before this one's pages are waited for.
+    struct Batch { int n, ph; };
+    DcWalk wn = w;
+    int off = 0;
+    auto fetch = [&]() {
+      Batch q = {0, 0};
+      if (wn.t >= wn.t_end) return q;
+      const int len = dc_segment_len(wn);
+      q.n = min(32, len - off);
+      if (lane < q.n) {
+        int page = c.block_table[size_t(wn.b) * c.max_pages_per_seq + min(wn.page + off + lane, c.max_pages_per_seq - 1)];
+        if (page < 0 || page >= c.num_pages) { atomicExch(c.status, kStatusBounds); page = 0; }
+        q.ph = page * c.n_kv + wn.kvh;
       }
-      dc_advance(c, w, len);
+      off += q.n;
+      if (off == len) {
+        dc_advance<kD8Gap>(c, wn, len);
+        off = 0;
+      }
+      return q;
+    };
+    bool ok = true;
+    int it = 0;                                                    // pages so far
+    auto copy = [&](int i, int ph) {                               // lane 0: page i of the CTA into its stage
+      const int st = i % kD8Stages;
+      if (!mbar_wait(&empty[st], ((i / kD8Stages) & 1) ^ 1)) return false;
+      mbar_add_tx(&full[st], 2 * SM::kTile);
+      tma_load_2d(smem + st * 2 * SM::kTile, &tmK, &full[st], 0, ph * 64);
+      tma_load_2d(smem + st * 2 * SM::kTile + SM::kTile, &tmV, &full[st], 0, ph * 64);
+      return true;
+    };
+    Batch cur = fetch();
+    while (ok && cur.n > 0) {
+      float sk = 0.f, sv = 1.f;
+      if (lane < cur.n) { sk = c.k_scales[cur.ph]; sv = c.v_scales[cur.ph]; }
+      const int early = min(cur.n, kD8Stages);
+      for (int j = 0; j < early && ok; ++j) {
+        const int ph = __shfl_sync(0xffffffffu, cur.ph, j);
+        if (lane == 0) ok = copy(it + j, ph);
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+      }
+      const Batch next = fetch();
+      // the places of these 32 pages in the ring of 64 were last read at least 32 - kD8Stages pages ago
+      if (lane < cur.n) scales[(it + lane) & 63] = make_float4(sk, c8_is_nan(sv) ? sv : float(c8_scale_exp(sv)), 1.f / sv, 0.f);
+      __syncwarp();
+      if (lane == 0 && ok)
+        for (int j = 0; j < early; ++j) mbar_arrive(&full[(it + j) % kD8Stages]);
+      for (int j = early; j < cur.n && ok; ++j) {
+        const int ph = __shfl_sync(0xffffffffu, cur.ph, j);
+        if (lane == 0) {
+          ok = copy(it + j, ph);
+          if (ok) mbar_arrive(&full[(it + j) % kD8Stages]);
+        }
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+      }
+      it += cur.n;
+      cur = next;
     }
     if (!ok && lane == 0) atomicExch(c.status, kStatusTimeout);
     return;
@@ -145,7 +170,7 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   // -------------------------------------------------------------------- consumers
   const int G = c.n_q / c.n_kv;
   const int g = lane >> 2, t4 = lane & 3;
-  const int wq = warp & 3, grp = warp >> 2;                        // quarter of a page, group of four warps
+  const int wq = warp;                                             // quarter of a page
   const int ctid = threadIdx.x;
   // MMA row i (0..7) of a group of 8 keys is key krow(i): rows 4 apart sit in different halves of the banks
   const int krow_g = ((g & 1) << 2) | (g >> 1);
@@ -153,15 +178,18 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   const int krow_l = ((l7 & 1) << 2) | (l7 >> 1);
   const uint32_t ring = smem_u32(smem);
   const uint32_t k_off = uint32_t(wq * 16 + krow_g) * 128 + (((t4 ^ krow_g) & 7) << 4);          // chunk t4 of the lane's first key
-  const uint32_t v_row = uint32_t(wq * 16 + ((lane >> 3) & 1) * 8 + krow_l) * 128;
-  const int v_ch = lane >> 4;                                      // ldmatrix: matrices 2 and 3 are the next chunk
+  // ldmatrix: this lane's row and chunk (matrices 2 and 3 are the next chunk); chunk pair cp is at ^ (cp << 5)
+  const uint32_t v_off = uint32_t(SM::kTile) + uint32_t(wq * 16 + ((lane >> 3) & 1) * 8 + krow_l) * 128 + (((lane >> 4) ^ krow_l) << 4);
   bool ok = true;
-  int it = 0;
+  int it = 0, st = 0;                                              // pages so far, their next stage and the parity of its phase
+  uint32_t ph = 0;
+  // pairs whose keys are split over CTAs: at most the CTA's first and its last; their tickets are taken at the end
+  int pend_b[2], pend_kvh[2], pend_c0[2], pend_n[2], n_pend = 0;
 
   while (w.t < w.t_end) {
     const int len = dc_segment_len(w);
     const int b = w.b, kvh = w.kvh, kv_len = w.kv_len;
-    const int pair_first = w.seq_first + kvh * w.np;
+    const int pair_first = dc_pair_first<kD8Gap>(w);
     const int c_first = pair_first / w.per;
     const int n_segs = (pair_first + w.np - 1) / w.per - c_first + 1;
     const int seg = int(blockIdx.x) - c_first;
@@ -213,17 +241,18 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     for (int n = 0; n < NT; ++n) { m_ref[n][0] = m_ref[n][1] = -INFINITY; l_run[n][0] = l_run[n][1] = 0.f; }
 
     for (int j = 0; j < len; ++j, ++it) {
-      if (CF::kGroups > 1 && (it & 1) != grp) continue;            // the other group's page
-      const int st = it % kD8Stages;
+      const int cur = st;
+      const uint32_t cur_ph = ph;
+      if (++st == kD8Stages) { st = 0; ph ^= 1; }
       // A wait that runs out ends this warp's work: it keeps walking the segments (so that it still meets the other
       // warps at every barrier and the tickets are taken) but waits for and computes nothing more.
-      if (ok && !mbar_wait(&full[st], (it / kD8Stages) & 1)) ok = false;
+      if (ok && !mbar_wait(&full[cur], cur_ph)) ok = false;
       if (!ok) continue;
       const int key0 = (w.page + j) * 64 + wq * 16;                // this warp's 16 keys of the page
       if (key0 < kv_len) {
-        const uint32_t k_base = ring + st * 2 * SM::kTile + k_off;
-        const uint32_t v_base = ring + st * 2 * SM::kTile + SM::kTile + v_row;
-        const float4 sc = scales[st];
+        const uint32_t k_base = ring + cur * 2 * SM::kTile + k_off;
+        const uint32_t v_base = ring + cur * 2 * SM::kTile + v_off;
+        const float4 sc = scales[it & 63];
         float s[NT][4];
 #pragma unroll
         for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
@@ -244,14 +273,21 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         bool grow = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
+          const float f0 = qs[n][0] * sc.x, f1 = qs[n][1] * sc.x;
+          if (LOGITS) {
+            float* lg = a.logits + (size_t(b) * c.n_q + kvh * G + n * 8 + t4 * 2) * a.logits_stride + key0 + krow_g;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float f = qs[n][e & 1] * sc.x;
-            const int key = key0 + krow_g + (e >> 1) * 8;
-            const bool valid = !tail || key < kv_len;
-            if (a.logits && valid && n * 8 + t4 * 2 + (e & 1) < G)
-              a.logits[(size_t(b) * c.n_q + kvh * G + n * 8 + t4 * 2 + (e & 1)) * a.logits_stride + key] = s[n][e] * f;
-            s[n][e] = valid ? fmaf(s[n][e], f, sc.y) : -INFINITY;
+            for (int e = 0; e < 4; ++e)
+              if (n * 8 + t4 * 2 + (e & 1) < G && key0 + krow_g + (e >> 1) * 8 < kv_len)
+                lg[(e & 1) * a.logits_stride + (e >> 1) * 8] = s[n][e] * ((e & 1) ? f1 : f0);
+          }
+          s[n][0] = fmaf(s[n][0], f0, sc.y);
+          s[n][1] = fmaf(s[n][1], f1, sc.y);
+          s[n][2] = fmaf(s[n][2], f0, sc.y);
+          s[n][3] = fmaf(s[n][3], f1, sc.y);
+          if (tail) {
+            if (key0 + krow_g >= kv_len) s[n][0] = s[n][1] = -INFINITY;
+            if (key0 + krow_g + 8 >= kv_len) s[n][2] = s[n][3] = -INFINITY;
           }
           grow = grow || fmaxf(s[n][0], s[n][2]) > m_ref[n][0] + kD8Lazy || fmaxf(s[n][1], s[n][3]) > m_ref[n][1] + kD8Lazy;
         }
@@ -295,7 +331,7 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
 #pragma unroll
         for (int cp = 0; cp < NC / 2; ++cp) {
           uint32_t v[4];
-          ldmatrix_x4_trans(v, v_base + ((((cp * 2 + v_ch) ^ krow_l) & 7) << 4));
+          ldmatrix_x4_trans(v, v_base ^ (cp << 5));
           if (tail) { v[0] &= keep0; v[1] &= keep1; v[2] &= keep0; v[3] &= keep1; }
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
@@ -308,7 +344,7 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         }
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(&empty[st]);                      // this warp is done with the stage
+      if (lane == 0) mbar_arrive(&empty[cur]);                     // this warp is done with the stage
     }
 
     // ---- the warps' states become one: common maximum, then the rescaled outputs are added in a fixed order
@@ -399,105 +435,122 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
           a.part_ml[(slot * 16 + r) * 2 + 1] = l;
         }
       }
+      pend_b[n_pend & 1] = b; pend_kvh[n_pend & 1] = kvh; pend_c0[n_pend & 1] = c_first; pend_n[n_pend & 1] = n_segs;
+      ++n_pend;
+    }
+    d8_bar<CT>();                                                  // mo and mm are free for the next segment
+    dc_advance<kD8Gap>(c, w, len);
+  }
+
+  // ---- tickets of the split pairs, and the merge of those this CTA is the last to finish
+  if (n_pend > 0) {
+    __threadfence();
+    d8_bar<CT>();
+    if (ctid < n_pend) {
+      const int q = ctid;
+      ticket_s[q] = atomicAdd(&a.split_done[pend_b[q] * c.n_kv + pend_kvh[q]], 1);
+    }
+    d8_bar<CT>();
+    for (int q = 0; q < n_pend; ++q) {
+      const int b = pend_b[q], kvh = pend_kvh[q], c_first = pend_c0[q], n_segs = pend_n[q];
+      if (ticket_s[q] != n_segs - 1) continue;
+      if (ctid == 0) a.split_done[b * c.n_kv + kvh] = 0;           // re-armed for the next call
       __threadfence();
-      d8_bar<CT>();
-      if (ctid == 0) *ticket_s = atomicAdd(&a.split_done[b * c.n_kv + kvh], 1);
-      d8_bar<CT>();
-      if (*ticket_s == n_segs - 1) {
-        if (ctid == 0) a.split_done[b * c.n_kv + kvh] = 0;         // re-armed for the next call
-        __threadfence();
-        // One warp per query head.  The segments' (m, l) are read one per lane and their outputs eight segments at a
-        // time; the sums run in segment order.  Segment s lives in slot 1 of CTA c_first (s = 0) or slot 0 of CTA
-        // c_first + s.
-        auto slot_of = [&](int s) { return s == 0 ? size_t(c_first) * 2 + 1 : size_t(c_first + s) * 2; };
-        for (int r = warp; r < G; r += CF::kWarps) {
-          float m = -INFINITY;
-          for (int s = lane; s < n_segs; s += 32) m = fmaxf(m, __ldcg(a.part_ml + (slot_of(s) * 16 + r) * 2));
+      // One warp per query head.  The segments' (m, l) are read one per lane and their outputs eight segments at a
+      // time; the sums run in segment order.  Segment s lives in slot 1 of CTA c_first (s = 0) or slot 0 of CTA
+      // c_first + s.
+      auto slot_of = [&](int s) { return s == 0 ? size_t(c_first) * 2 + 1 : size_t(c_first + s) * 2; };
+      for (int r = warp; r < G; r += CF::kWarps) {
+        float m = -INFINITY;
+        for (int s = lane; s < n_segs; s += 32) m = fmaxf(m, __ldcg(a.part_ml + (slot_of(s) * 16 + r) * 2));
 #pragma unroll
-          for (int o2 = 16; o2 > 0; o2 >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o2));
-          float acc[DH / 32];
+        for (int o2 = 16; o2 > 0; o2 >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o2));
+        float acc[DH / 32];
 #pragma unroll
-          for (int q = 0; q < DH / 32; ++q) acc[q] = 0.f;
-          float l = 0.f;
-          for (int c0 = 0; c0 < n_segs; c0 += 32) {
-            const int n = min(32, n_segs - c0);
-            float fs = 0.f, ls = 0.f;                              // lane s: factor and row sum of segment c0 + s
-            if (lane < n) {
-              const float ms = __ldcg(a.part_ml + (slot_of(c0 + lane) * 16 + r) * 2);
-              fs = ms == -INFINITY ? 0.f : fast_exp2(ms - m);
-              ls = __ldcg(a.part_ml + (slot_of(c0 + lane) * 16 + r) * 2 + 1);
-            }
-            for (int u0 = 0; u0 < n; u0 += 8) {
-              float v[8][DH / 32];
+        for (int i = 0; i < DH / 32; ++i) acc[i] = 0.f;
+        float l = 0.f;
+        for (int c0 = 0; c0 < n_segs; c0 += 32) {
+          const int n = min(32, n_segs - c0);
+          float fs = 0.f, ls = 0.f;                                // lane s: factor and row sum of segment c0 + s
+          if (lane < n) {
+            const float ms = __ldcg(a.part_ml + (slot_of(c0 + lane) * 16 + r) * 2);
+            fs = ms == -INFINITY ? 0.f : fast_exp2(ms - m);
+            ls = __ldcg(a.part_ml + (slot_of(c0 + lane) * 16 + r) * 2 + 1);
+          }
+          for (int u0 = 0; u0 < n; u0 += 8) {
+            float v[8][DH / 32];
 #pragma unroll
-              for (int u = 0; u < 8; ++u)
+            for (int u = 0; u < 8; ++u)
 #pragma unroll
-                for (int q = 0; q < DH / 32; ++q)
-                  v[u][q] = u0 + u < n ? __ldcg(a.part_o + (slot_of(c0 + u0 + u) * 16 + r) * DH + q * 32 + lane) : 0.f;
+              for (int i = 0; i < DH / 32; ++i)
+                v[u][i] = u0 + u < n ? __ldcg(a.part_o + (slot_of(c0 + u0 + u) * 16 + r) * DH + i * 32 + lane) : 0.f;
 #pragma unroll
-              for (int u = 0; u < 8; ++u) {
-                const float fu = __shfl_sync(0xffffffffu, fs, (u0 + u) & 31);   // (0 past the last segment)
-                const float lu = __shfl_sync(0xffffffffu, ls, (u0 + u) & 31);
-                l += fu * lu;
+            for (int u = 0; u < 8; ++u) {
+              const float fu = __shfl_sync(0xffffffffu, fs, (u0 + u) & 31);   // (0 past the last segment)
+              const float lu = __shfl_sync(0xffffffffu, ls, (u0 + u) & 31);
+              l += fu * lu;
 #pragma unroll
-                for (int q = 0; q < DH / 32; ++q) acc[q] += fu * v[u][q];
-              }
+              for (int i = 0; i < DH / 32; ++i) acc[i] += fu * v[u][i];
             }
           }
-          const float inv = 1.f / l;
-          __nv_bfloat16* dst = a.out + (long long)b * a.out_stride + (kvh * G + r) * c.dh;
-#pragma unroll
-          for (int q = 0; q < DH / 32; ++q)
-            if (q * 32 + lane < c.dh) dst[q * 32 + lane] = __float2bfloat16_rn(acc[q] * inv);
-          if (lane == 0 && a.lse) a.lse[size_t(b) * c.n_q + kvh * G + r] = m - kD8Shift + log2f(l);
         }
+        const float inv = 1.f / l;
+        __nv_bfloat16* dst = a.out + (long long)b * a.out_stride + (kvh * G + r) * c.dh;
+#pragma unroll
+        for (int i = 0; i < DH / 32; ++i)
+          if (i * 32 + lane < c.dh) dst[i * 32 + lane] = __float2bfloat16_rn(acc[i] * inv);
+        if (lane == 0 && a.lse) a.lse[size_t(b) * c.n_q + kvh * G + r] = m - kD8Shift + log2f(l);
       }
     }
-    d8_bar<CT>();                                                  // mo, mm, ticket_s are free for the next segment
-    dc_advance(c, w, len);
   }
   if (!ok && lane == 0) atomicExch(c.status, kStatusTimeout);
 }
 
 // two slots of 16 rows for each CTA that can run
-size_t cache8_decode_part_rows(int n_sms) { return size_t(2) * n_sms * 2 * 16; }
+size_t cache8_decode_part_rows(int n_sms) { return size_t(3) * n_sms * 2 * 16; }
 
 template <int FMT, int DH, int NT>
 static cudaError_t configure_t() {
-  return cudaFuncSetAttribute(cache8_decode_kernel<FMT, DH, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(D8Smem<DH, NT>::kBytes));
+  const cudaError_t e = cudaFuncSetAttribute(cache8_decode_kernel<FMT, DH, NT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(D8Smem<DH, NT>::kBytes));
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(cache8_decode_kernel<FMT, DH, NT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(D8Smem<DH, NT>::kBytes));
+}
+
+template <int FMT>
+static cudaError_t configure_format() {
+  cudaError_t e = configure_t<FMT, 64, 1>();
+  if (e == cudaSuccess) e = configure_t<FMT, 64, 2>();
+  if (e == cudaSuccess) e = configure_t<FMT, 128, 1>();
+  if (e == cudaSuccess) e = configure_t<FMT, 128, 2>();
+  return e;
 }
 
 cudaError_t cache8_decode_configure() {
-  cudaError_t e = configure_t<kC8E4M3, 64, 1>();
-  if (e == cudaSuccess) e = configure_t<kC8E4M3, 64, 2>();
-  if (e == cudaSuccess) e = configure_t<kC8E4M3, 128, 1>();
-  if (e == cudaSuccess) e = configure_t<kC8E4M3, 128, 2>();
-  if (e == cudaSuccess) e = configure_t<kC8Int8, 64, 1>();
-  if (e == cudaSuccess) e = configure_t<kC8Int8, 64, 2>();
-  if (e == cudaSuccess) e = configure_t<kC8Int8, 128, 1>();
-  if (e == cudaSuccess) e = configure_t<kC8Int8, 128, 2>();
-  return e;
+  const cudaError_t e = configure_format<kC8E4M3>();
+  return e != cudaSuccess ? e : configure_format<kC8Int8>();
 }
 
 template <int FMT, int DH, int NT>
 static void launch_decode_t(const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a, int n_sms, cudaStream_t st) {
   constexpr size_t smem = D8Smem<DH, NT>::kBytes;
-  static_assert(2 * (smem + 1024) <= 228 * 1024, "two CTAs per SM");
+  constexpr int kCtas = D8Cfg<NT>::kCtas;
+  static_assert(kCtas * (smem + 1024) <= 228 * 1024, "CTAs per SM");
   const long long most = ((long long)a.c.n_seqs * a.c.n_kv * a.c.max_kv_pages + kD8MinTiles - 1) / kD8MinTiles;
-  const int grid = int(most < 2LL * n_sms ? (most < 1 ? 1 : most) : 2LL * n_sms);
-  launch_pdl(cache8_decode_kernel<FMT, DH, NT>, dim3(grid), dim3(D8Cfg<NT>::kThreads), smem, st, tmK, tmV, a);
+  const int grid = int(most < (long long)kCtas * n_sms ? (most < 1 ? 1 : most) : (long long)kCtas * n_sms);
+  launch_pdl(a.logits ? cache8_decode_kernel<FMT, DH, NT, true> : cache8_decode_kernel<FMT, DH, NT, false>, dim3(grid), dim3(D8Cfg<NT>::kThreads), smem, st, tmK, tmV, a);
+}
+
+template <int FMT>
+static void launch_decode_format(const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a, int n_sms, cudaStream_t st) {
+  const bool wide = a.c.n_q / a.c.n_kv > 8;
+  if (a.c.dh > 64) wide ? launch_decode_t<FMT, 128, 2>(tmK, tmV, a, n_sms, st) : launch_decode_t<FMT, 128, 1>(tmK, tmV, a, n_sms, st);
+  else wide ? launch_decode_t<FMT, 64, 2>(tmK, tmV, a, n_sms, st) : launch_decode_t<FMT, 64, 1>(tmK, tmV, a, n_sms, st);
 }
 
 void launch_cache8_decode(int fmt, const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a, int n_sms, cudaStream_t st) {
   if (a.c.n_seqs <= 0) return;
-  const bool wide = a.c.n_q / a.c.n_kv > 8, big = a.c.dh > 64;
-  if (fmt == kC8E4M3) {
-    if (big) wide ? launch_decode_t<kC8E4M3, 128, 2>(tmK, tmV, a, n_sms, st) : launch_decode_t<kC8E4M3, 128, 1>(tmK, tmV, a, n_sms, st);
-    else wide ? launch_decode_t<kC8E4M3, 64, 2>(tmK, tmV, a, n_sms, st) : launch_decode_t<kC8E4M3, 64, 1>(tmK, tmV, a, n_sms, st);
-  } else {
-    if (big) wide ? launch_decode_t<kC8Int8, 128, 2>(tmK, tmV, a, n_sms, st) : launch_decode_t<kC8Int8, 128, 1>(tmK, tmV, a, n_sms, st);
-    else wide ? launch_decode_t<kC8Int8, 64, 2>(tmK, tmV, a, n_sms, st) : launch_decode_t<kC8Int8, 64, 1>(tmK, tmV, a, n_sms, st);
-  }
+  if (fmt == kC8E4M3) launch_decode_format<kC8E4M3>(tmK, tmV, a, n_sms, st);
+  else launch_decode_format<kC8Int8>(tmK, tmV, a, n_sms, st);
 }
 
 }  // namespace foe

@@ -1,6 +1,8 @@
 // How the persistent CTAs of a decode attention kernel divide the call's pages: the pages of all (sequence, KV head)
 // pairs form one list (sequence-major, then KV head, then page) of T entries and CTA c takes the entries
-// [c * per, (c + 1) * per), per = max(min_tiles, ceil(T / grid)).  Args: context_lens, n_seqs, n_kv, max_kv_pages.
+// [c * per, (c + 1) * per), per = max(min_tiles, ceil(T / grid)).  GAP: entries without a page in front of every pair,
+// which stand for the time that starting a pair costs, so that a CTA whose range holds more pairs gets fewer pages.
+// Args: context_lens, n_seqs, n_kv, max_kv_pages.
 #pragma once
 
 #include "common.cuh"
@@ -11,7 +13,7 @@ namespace foe {
 struct DcWalk {
   int b, kvh, page;      // current entry
   int np, kv_len;        // pages and keys (cached + the new token) of sequence b
-  int seq_first;         // list index of the first page of sequence b
+  int seq_first;         // list index of the first entry of sequence b
   int t, t_end;          // current list index, end of this CTA's range
   int per;
 };
@@ -24,7 +26,7 @@ __device__ __forceinline__ int dc_pages(const Args& a, int b, int* kv_len) {
 }
 
 // Every warp works this out for itself (all 32 lanes): the CTA's range and where it starts.  False: nothing to do.
-template <typename Args>
+template <int GAP = 0, typename Args>
 __device__ __forceinline__ bool dc_begin(const Args& a, int min_tiles, DcWalk& w) {
   const int lane = threadIdx.x & 31;
   int sum = 0, np_first = 0, kl_first = 0;        // (the first 32 sequences' values are kept for the search below)
@@ -32,7 +34,7 @@ __device__ __forceinline__ bool dc_begin(const Args& a, int min_tiles, DcWalk& w
     int kl = 0;
     const int np = b0 + lane < a.n_seqs ? dc_pages(a, b0 + lane, &kl) : 0;
     if (b0 == 0) { np_first = np; kl_first = kl; }
-    sum += np;
+    sum += np + (np > 0 ? GAP : 0);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -42,18 +44,19 @@ __device__ __forceinline__ bool dc_begin(const Args& a, int min_tiles, DcWalk& w
   if (t0 >= T) return false;
   w.t = int(t0);
   w.t_end = min(T, w.t + w.per);
-  int base = 0;                                  // pages of the sequences before this chunk of 32
+  int base = 0;                                  // entries (per KV head) of the sequences before this chunk of 32
   for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
     int kl = kl_first;
     const int np = b0 == 0 ? np_first : (b0 + lane < a.n_seqs ? dc_pages(a, b0 + lane, &kl) : 0);
-    int incl = np;
+    const int size = np + (np > 0 ? GAP : 0);
+    int incl = size;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int v = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += v;
     }
-    const int first = a.n_kv * (base + incl - np);
-    const bool hit = np > 0 && w.t >= first && w.t < first + a.n_kv * np;
+    const int first = a.n_kv * (base + incl - size);
+    const bool hit = np > 0 && w.t >= first && w.t < first + a.n_kv * size;
     const uint32_t m = __ballot_sync(0xffffffffu, hit);
     if (m) {
       const int src = __ffs(m) - 1;
@@ -62,9 +65,13 @@ __device__ __forceinline__ bool dc_begin(const Args& a, int min_tiles, DcWalk& w
       w.np = __shfl_sync(0xffffffffu, np, src);
       w.kv_len = __shfl_sync(0xffffffffu, kl, src);
       const int rem = w.t - w.seq_first;
-      w.kvh = rem / w.np;
-      w.page = rem - w.kvh * w.np;
-      return true;
+      w.kvh = rem / (w.np + GAP);
+      w.page = rem - w.kvh * (w.np + GAP) - GAP;
+      if (GAP > 0 && w.page < 0) {                 // the range starts in front of a pair
+        w.t -= w.page;
+        w.page = 0;
+      }
+      return GAP == 0 || w.t < w.t_end;
     }
     base += __shfl_sync(0xffffffffu, incl, 31);
   }
@@ -74,16 +81,21 @@ __device__ __forceinline__ bool dc_begin(const Args& a, int min_tiles, DcWalk& w
 // pages of the segment that starts at the current entry
 __device__ __forceinline__ int dc_segment_len(const DcWalk& w) { return min(w.np - w.page, w.t_end - w.t); }
 
-template <typename Args>
+// list index of the first page of the current pair
+template <int GAP = 0>
+__device__ __forceinline__ int dc_pair_first(const DcWalk& w) { return w.seq_first + w.kvh * (w.np + GAP) + GAP; }
+
+template <int GAP = 0, typename Args>
 __device__ __forceinline__ void dc_advance(const Args& a, DcWalk& w, int len) {
   w.t += len;
   w.page += len;
   if (w.page >= w.np) {
     w.page = 0;
     w.kvh += 1;
+    w.t += GAP;
     if (w.kvh == a.n_kv) {
       w.kvh = 0;
-      w.seq_first += a.n_kv * w.np;
+      w.seq_first += a.n_kv * (w.np + GAP);
       w.b += 1;
       if (w.t < w.t_end) w.np = dc_pages(a, w.b, &w.kv_len);
     }
