@@ -83,5 +83,6 @@ size_t cache8_chunk_part_rows(int n_sms);
 cudaError_t cache8_chunk_configure();
 void launch_cache8_weights(int fmt, const Cache8WeightsArgs& w, cudaStream_t st);
 void launch_cache8_evict(int fmt, const Cache8EvictArgs& a, cudaStream_t st);
+cudaError_t cache8_evict_configure();
 
 }  // namespace foe

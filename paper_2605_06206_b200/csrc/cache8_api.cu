@@ -220,7 +220,7 @@ foe_status foe_cache_create(const foe_cache_config* cfg, foe_cache** out) {
       cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return FOE_ERR_CUDA;
   if (major != 10) return FOE_ERR_UNSUPPORTED;            // tcgen05 kernels: sm_100 only
-  if (cache8_decode_configure() != cudaSuccess || cache8_chunk_configure() != cudaSuccess) { cudaGetLastError(); return FOE_ERR_CUDA; }
+  if (cache8_decode_configure() != cudaSuccess || cache8_chunk_configure() != cudaSuccess || cache8_evict_configure() != cudaSuccess) { cudaGetLastError(); return FOE_ERR_CUDA; }
   foe_cache* h = new (std::nothrow) foe_cache();
   if (!h) return FOE_ERR_OOM;
   h->cfg = *cfg;
