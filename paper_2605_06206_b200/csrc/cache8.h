@@ -3,6 +3,7 @@
 
 #include <cuda.h>
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -42,6 +43,7 @@ struct Cache8AttendArgs {
   // partial results of a (sequence, KV head) whose keys are worked on by several CTAs
   float *part_o, *part_ml;
   int* split_done;
+  int* division;                    // chunks: first CTA of every block of a launch that splits keys
   // for the accumulated weights (nullptr without them)
   float* lse;                       // [n_tokens][n_q] log2 of the row's softmax denominator
   float* logits;                    // single tokens: [n_seqs][n_q][logits_stride] scores in the log2 domain
@@ -75,10 +77,21 @@ void launch_cache8_decode(int fmt, const CUtensorMap& tmK, const CUtensorMap& tm
                           cudaStream_t st);
 size_t cache8_decode_part_rows(int n_sms);   // rows of part_o / part_ml
 cudaError_t cache8_decode_configure();
-// chunks: q_lens given, n_tokens rows in all.  part_o / part_ml hold cache8_chunk_part_rows(n_sms) rows.
-// Returns the number of kernels launched.
-int launch_cache8_chunk(int fmt, const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a, int n_sms,
-                         cudaStream_t st);
+// Operand tiles of long chunks' sequences: K bf16, V fp16 [pages][n_kv][64][dh padded to 64 or 128], with their scales and maps
+// (64 x 64 boxes).  pages is at least what the longest sequence of a call needs.
+struct Cache8Workspace {
+  __nv_bfloat16* k;
+  __half* v;
+  float4* scales;
+  long long pages;
+  CUtensorMap tmK, tmV;
+};
+// chunks: q_lens given, n_tokens rows in all; tmQ maps q as [tokens][heads][dh] with boxes of 128 x 1 x 64.  part_o / part_ml hold cache8_chunk_part_rows(n_sms) rows; ws is used by calls
+// with max_q_len >= cache8_expand_min_tokens(n_q / n_kv, dh).  Returns the number of kernels launched.
+int launch_cache8_chunk(int fmt, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a,
+                        const Cache8Workspace& ws, int n_sms, cudaStream_t st);
+int cache8_expand_min_tokens(int group, int dh);    // group: query heads per KV head
+int cache8_chunk_division_ints();
 size_t cache8_chunk_part_rows(int n_sms);
 cudaError_t cache8_chunk_configure();
 void launch_cache8_weights(int fmt, const Cache8WeightsArgs& w, cudaStream_t st);

@@ -33,10 +33,17 @@ void lay_out(foe_cache* h, Arena* m) {
   m->take(&h->status, 1);                                  // zeroed at creation, with split_done behind it
   m->take(&h->split_done, h->split_done_count);
   m->take(&h->part_ml, rows * 2);
+  m->take(&h->division, cache8_chunk_division_ints());
   m->take(&h->part_o, rows * dhp);
   if (c.track_weights) {
     m->take(&h->lse, size_t(h->rows_max) * c.n_q_heads);
     m->take(&h->logits, size_t(c.max_seqs) * c.n_q_heads * size_t(h->logits_stride));
+  }
+  if (h->ws.pages) {
+    const size_t tiles = size_t(h->ws.pages) * c.n_kv_heads;
+    m->take(&h->ws.scales, tiles);
+    m->take(&h->ws.k, tiles * 64 * dhp);
+    m->take(&h->ws.v, tiles * 64 * dhp);
   }
   if (c.for_layers) {
     const size_t stage = (size_t(h->rows_max) + 63) / 64 * 64 * c.n_kv_heads * c.head_dim;
@@ -59,9 +66,33 @@ bool make_code_map(CUtensorMap* m, const void* base, uint64_t rows, uint64_t dh)
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// 16-bit operand tiles: rows of `width` values, a box is 64 rows of 64 of them
+bool make_tile_map(CUtensorMap* m, CUtensorMapDataType type, const void* base, uint64_t rows, uint64_t width) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (!fn) return false;
+  const cuuint64_t gdim[2] = {width, rows};
+  const cuuint64_t gstride[1] = {width * 2};
+  const cuuint32_t box[2] = {64, 64};
+  const cuuint32_t estr[2] = {1, 1};
+  return fn(m, type, 2, const_cast<void*>(base), gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// queries [tokens][heads][dh], a box is 64 columns of one head for 128 tokens (columns behind dh are zeros)
+bool make_query_map(CUtensorMap* m, const void* base, uint64_t tokens, uint64_t heads, uint64_t dh, uint64_t stride, uint64_t head_stride) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (!fn) return false;
+  const cuuint64_t gdim[3] = {dh, heads, tokens};
+  const cuuint64_t gstride[2] = {head_stride * 2, stride * 2};
+  const cuuint32_t box[3] = {64, 1, 128};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 foe_status check_config(const foe_cache_config* c) {
   if (c->n_q_heads <= 0 || c->n_kv_heads <= 0 || c->n_q_heads % c->n_kv_heads || c->n_q_heads / c->n_kv_heads > 16) return FOE_ERR_CONFIG;
-  if (c->n_kv_heads > 65535) return FOE_ERR_CONFIG;
+  if (c->n_kv_heads > 16384) return FOE_ERR_CONFIG;
   if (c->head_dim != 64 && c->head_dim != 96 && c->head_dim != 128) return FOE_ERR_CONFIG;
   if (c->page_size != 64 || (c->format != FOE_CACHE_E4M3 && c->format != FOE_CACHE_INT8)) return FOE_ERR_CONFIG;
   if (c->max_tokens <= 0 || c->max_seqs <= 0 || c->max_seqs > 65535 || c->max_context <= 0) return FOE_ERR_CONFIG;
@@ -136,14 +167,19 @@ int cache8_attend(foe_cache* h, const foe_cache_view* v, const void* q, long lon
   a.q = static_cast<const __nv_bfloat16*>(q); a.q_stride = q_stride; a.q_head_stride = q_head_stride;
   a.out = static_cast<__nv_bfloat16*>(out); a.out_stride = out_stride;
   a.scale_log2 = float(1.4426950408889634 / sqrt(double(a.c.dh)));
-  a.part_o = h->part_o; a.part_ml = h->part_ml; a.split_done = h->split_done;
+  a.part_o = h->part_o; a.part_ml = h->part_ml; a.split_done = h->split_done; a.division = h->division;
   if (w_out) { a.lse = h->lse; a.logits = h->logits; a.logits_stride = h->logits_stride; }
   const uint64_t rows = uint64_t(a.c.num_pages) * a.c.n_kv * 64;
   CUtensorMap tmK, tmV;
   if (!make_code_map(&tmK, v->k_pages, rows, a.c.dh) || !make_code_map(&tmV, v->v_pages, rows, a.c.dh)) return -1;
   int n = 1;
-  if (!v->q_lens) launch_cache8_decode(h->cfg.format, tmK, tmV, a, h->n_sms, st);
-  else n = launch_cache8_chunk(h->cfg.format, tmK, tmV, a, h->n_sms, st);
+  if (!v->q_lens) {
+    launch_cache8_decode(h->cfg.format, tmK, tmV, a, h->n_sms, st);
+  } else {
+    CUtensorMap tmQ = tmK;                       // (only long chunks read their queries through a map)
+    if (h->ws.pages && a.c.n_tokens > 0 && !make_query_map(&tmQ, q, a.c.n_tokens, a.c.n_q, a.c.dh, q_stride, q_head_stride)) return -1;
+    n = launch_cache8_chunk(h->cfg.format, tmQ, tmK, tmV, a, h->ws, h->n_sms, st);
+  }
   if (w_out) {
     Cache8WeightsArgs w;
     w.a = a; w.weights_in = w_in; w.weights_out = w_out; w.weights_stride = w_stride; w.window = window;
@@ -229,6 +265,14 @@ foe_status foe_cache_create(const foe_cache_config* cfg, foe_cache** out) {
   h->rows_max = cfg->max_tokens > cfg->max_seqs ? cfg->max_tokens : cfg->max_seqs;
   h->split_done_count = size_t(cfg->max_seqs) * cfg->n_kv_heads;
   h->logits_stride = ((long long)cfg->max_context + 63) / 64 * 64;
+  if (cfg->max_tokens >= cache8_expand_min_tokens(cfg->n_q_heads / cfg->n_kv_heads, cfg->head_dim)) {
+    // room for every sequence of a call, but no more than kExpandBytes unless one sequence needs it
+    constexpr size_t kExpandBytes = size_t(256) << 20;
+    const long long one = h->logits_stride / 64, all = one * cfg->max_seqs;
+    const long long fit = (long long)(kExpandBytes / (size_t(cfg->n_kv_heads) * 2 * 64 * (cfg->head_dim > 64 ? 128 : 64) * 2));
+    h->ws.pages = all < fit ? all : (one > fit ? one : fit);
+    if (h->ws.pages * cfg->n_kv_heads * 64 >= (1LL << 31)) { delete h; return FOE_ERR_CONFIG; }
+  }
   Arena sizes;
   lay_out(h, &sizes);
   Arena mem;
@@ -239,6 +283,14 @@ foe_status foe_cache_create(const foe_cache_config* cfg, foe_cache** out) {
   }
   h->memory = mem.base;
   lay_out(h, &mem);
+  if (h->ws.pages) {
+    const uint64_t rows = uint64_t(h->ws.pages) * cfg->n_kv_heads * 64;
+    const uint64_t width = cfg->head_dim > 64 ? 128 : 64;
+    if (!make_tile_map(&h->ws.tmK, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, h->ws.k, rows, width) || !make_tile_map(&h->ws.tmV, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, h->ws.v, rows, width)) {
+      foe_cache_destroy(h);
+      return FOE_ERR_CUDA;
+    }
+  }
   const size_t zeroed = reinterpret_cast<uint8_t*>(h->part_ml) - mem.base;
   if (cudaMemset(mem.base, 0, zeroed) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
     cudaGetLastError();

@@ -7,12 +7,12 @@
 //   * K and V pages arrive as codes (TMA, half the bytes) and four converter warps turn them into fp16 operand tiles
 //     in the 128-byte-swizzled layout, exactly and unscaled.  The page's K scale multiplies the scores and its V scale
 //     enters the exponent, t = s + log2(scale_v); the row sum takes it back out.
-//   * Q becomes fp16 once per CTA: a power of two per row brings the row's largest element to [2^7, 2^8), which keeps
+//   * Q becomes fp16 once per CTA (long chunks, whose K tiles are expanded to bf16 beforehand, keep it as it is): a power of two per row brings the row's largest element to [2^7, 2^8), which keeps
 //     every bf16 value within 2^31 of it (the factor joins the K scale).  P is fp16 too (11 bits where bf16 has 8),
 //     kept 2^6 above its natural scale so that only probabilities below 2^-30 of the largest are lost.
 //   * K and V tiles have rings of their own: a K tile is free as soon as its scores exist, so the converters run ahead.
-//   * Calls with few query rows split the keys over CTAs; each split leaves (m, l, unnormalised O) and a second kernel
-//     joins them in order.
+//   * Calls with few query blocks split their keys over CTAs, as evenly as the call's lengths allow; each split leaves
+//     (m, l, unnormalised O) and a second kernel joins them in order.
 // Warp roles (768 threads): warp 0 TMA producer, warps 1 and 2 MMA issuers (one per head), warps 4-7 converters, warps
 // 8-23 softmax.
 #include <math.h>
@@ -24,14 +24,19 @@
 namespace foe {
 
 constexpr int kC8Rows = 128, kC8Keys = 64;
-constexpr int kC8Threads = 768;
-constexpr int kC8Raw = 3, kC8Ring = 3;            // stages of codes; operand tiles of K and of V
 constexpr int kC8Scales = 16;                     // ring of the steps' scales (further ahead than the producer can be)
-constexpr int kC8SoftWarp = 8;                    // first softmax warp
-// Registers: the block is launched with kC8RegsLaunch each; warpgroup 0 and the converters hand back what the four
-// softmax warpgroups take (setmaxnreg.inc would wait forever for more than that).
-constexpr int kC8RegsLaunch = 80, kC8RegsLow = 24, kC8RegsConv = 40, kC8RegsHigh = 104;
-static_assert(128 * (kC8RegsLow + kC8RegsConv) + 512 * kC8RegsHigh <= kC8Threads * kC8RegsLaunch, "softmax warpgroups would wait for registers forever");
+// Registers: the block is launched with kRegsLaunch each; the warpgroups in front of the softmax hand back what its four
+// take (setmaxnreg.inc would wait forever for more than that).
+template <bool EXPANDED>
+struct C8Cfg {
+  static constexpr int kThreads = EXPANDED ? 640 : 768;
+  static constexpr int kSoftWarp = EXPANDED ? 4 : 8;               // first softmax warp
+  static constexpr int kRaw = EXPANDED ? 0 : 3;                    // stages of codes
+  static constexpr int kRing = EXPANDED ? 4 : 3;                   // operand tiles of K and of V
+  static constexpr int kFullCount = EXPANDED ? 1 : 4;              // arrivals that fill a tile: the copy's, or the converters'
+  static constexpr int kRegsLaunch = EXPANDED ? 96 : 80, kRegsLow = EXPANDED ? 32 : 24, kRegsConv = 40, kRegsHigh = EXPANDED ? 112 : 104;
+  static_assert(128 * (kRegsLow + (EXPANDED ? 0 : kRegsConv)) + 512 * kRegsHigh <= kThreads * kRegsLaunch, "softmax warpgroups would wait for registers forever");
+};
 constexpr float kC8Shift = 6.f;
 
 __device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -40,16 +45,17 @@ __host__ __device__ constexpr uint32_t umma_idesc_f16(int M, int N) {
   return (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
 }
 
-template <int DH>
+template <int DH, bool EXPANDED>
 struct C8Smem {
+  using CF = C8Cfg<EXPANDED>;
   static constexpr int kQTile = kC8Rows * DH * 2;
   static constexpr int kTile = kC8Keys * DH * 2;               // one fp16 operand tile
   static constexpr int kRawTile = kC8Keys * 128;               // codes, rows padded to 128 bytes by the TMA box
   static constexpr int kQOff = 0;
   static constexpr int kKOff = 2 * kQTile;
-  static constexpr int kVOff = kKOff + kC8Ring * kTile;
-  static constexpr int kRawOff = kVOff + kC8Ring * kTile;
-  static constexpr int kBarOff = kRawOff + kC8Raw * 2 * kRawTile;
+  static constexpr int kVOff = kKOff + CF::kRing * kTile;
+  static constexpr int kRawOff = kVOff + CF::kRing * kTile;
+  static constexpr int kBarOff = kRawOff + CF::kRaw * 2 * kRawTile;
   static constexpr int kScaleOff = kBarOff + 384;              // [kC8Scales] (K scale, log2 V scale, 1 / V scale, -)
   static constexpr int kHandOff = kScaleOff + kC8Scales * 16;  // [2 tiles][128 rows][2]
   static constexpr int kRedOff = kHandOff + 2 * kC8Rows * 2 * 4;
@@ -59,13 +65,77 @@ struct C8Smem {
 // query heads a CTA works on: two that share a KV head, or one where the group is odd
 __device__ __forceinline__ int c8_heads_per_block(const Cache8Args& c) { return (c.n_q / c.n_kv) % 2 == 0 ? 2 : 1; }
 
-template <int FMT, int DH>
-__global__ void __launch_bounds__(kC8Threads, 1)
-cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const Cache8AttendArgs a,
-                    const int q_blocks, const int n_splits) {
+// What one launch covers: query blocks of every sequence, whether their keys are split, and the sequences whose chunk has at
+// least min_q and fewer than end_q tokens (a call may run its long chunks one way and its short ones another); with
+// EXPANDED also the first sequence and their number, whose operand tiles and scales are in the workspace.
+struct C8Launch {
+  int q_blocks, min_q, end_q;
+  int split;                       // 0: one CTA per block; 1: the keys of a block are split over CTAs (c8_divide)
+  int seq0, n_seqs;
+  int ws_pages;                    // EXPANDED: pages of a sequence in the workspace
+  const float4* ws_scales;         // [sequence - seq0][ws_pages][n_kv] (K scale, log2 V scale, 1 / V scale, -)
+};
+
+// A launch of fewer blocks than SMs gives every block as many CTAs as keep the longest of them short: `per` is the
+// smallest number of steps (at least kC8MinSteps) for which sum_i ceil(steps_i / per) CTAs fit the grid, and block i's
+// CTAs are first[i] .. first[i + 1] - 1.  Worked out by one warp of every CTA from the lengths on the device; the first CTA
+// leaves it for the joining kernel.
+constexpr int kC8MaxSplitBlocks = 256, kC8MinSteps = 4;
+struct C8Division { int per, first[kC8MaxSplitBlocks + 1]; };
+__device__ __forceinline__ void c8_block_of(const Cache8Args& c, const C8Launch& lc, int pairs, int lin, int& b, int& pair, int& q0) {
+  const int per_qb = pairs * lc.n_seqs;
+  q0 = (lc.q_blocks - 1 - lin / per_qb) * kC8Rows;         // late query blocks (long causal extents) of the whole call first
+  pair = (lin % per_qb) % pairs;
+  b = lc.seq0 + (lin % per_qb) / pairs;
+}
+__device__ __forceinline__ void c8_divide(const Cache8Args& c, const C8Launch& lc, int pairs, int n_blocks, int n_ctas, C8Division* d) {
+  const int lane = threadIdx.x & 31;
+  int most = 0;
+  for (int i = lane; i < n_blocks; i += 32) {
+    int b, pair, q0, steps = 0;
+    c8_block_of(c, lc, pairs, i, b, pair, q0);
+    const int q_len = c.q_lens[b], ctx = c.context_lens[b];
+    const bool bad = q_len < 0 || q_len > c.max_q_len || ctx < 0 || (long long)ctx + q_len > c.max_len;
+    if (bad && blockIdx.x == 0) atomicExch(c.status, kStatusBounds);
+    if (!bad && q_len >= lc.min_q && q_len < lc.end_q && q0 < q_len)
+      steps = (ctx + min(q0 + kC8Rows, q_len) + kC8Keys - 1) / kC8Keys;
+    d->first[i] = steps;
+    most = max(most, steps);
+  }
+  __syncwarp();
+  most = __reduce_max_sync(0xffffffffu, most);
+  int lo = kC8MinSteps, hi = max(most, kC8MinSteps);       // smallest `per` in [lo, hi] that fits (hi does: one CTA a block)
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    int n = 0;
+    for (int i = lane; i < n_blocks; i += 32) n += (d->first[i] + mid - 1) / mid;
+    if (__reduce_add_sync(0xffffffffu, n) <= n_ctas) hi = mid; else lo = mid + 1;
+  }
+  int base = 0;
+  for (int i0 = 0; i0 < n_blocks; i0 += 32) {
+    const int n = i0 + lane < n_blocks ? (d->first[i0 + lane] + lo - 1) / lo : 0;
+    int incl = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += v;
+    }
+    __syncwarp();
+    if (i0 + lane < n_blocks) d->first[i0 + lane] = base + incl - n;
+    base += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  if (lane == 0) { d->first[n_blocks] = base; d->per = lo; }
+}
+
+template <int FMT, int DH, bool EXPANDED>
+__global__ void __launch_bounds__(C8Cfg<EXPANDED>::kThreads, 1)
+cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                    const Cache8AttendArgs a, const C8Launch lc) {
   pdl_wait();
   pdl_launch_dependents();
-  using L = C8Smem<DH>;
+  using CF = C8Cfg<EXPANDED>;
+  using L = C8Smem<DH, EXPANDED>;
+  constexpr int kC8Raw = EXPANDED ? 1 : CF::kRaw, kC8Ring = CF::kRing;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBarOff);
@@ -89,23 +159,38 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   const Cache8Args& c = a.c;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  // Blocks start in the order of their linear index: late query blocks (long causal extents) of the whole call first.
+  // Blocks start in the order of their linear index.
   const int n_tiles_q = c8_heads_per_block(c);
   const int pairs = c.n_q / n_tiles_q;
-  const int split = blockIdx.x % n_splits;
-  const int lin = blockIdx.x / n_splits;
-  const int per_qb = pairs * c.n_seqs;
-  const int qb = q_blocks - 1 - lin / per_qb;
-  const int pair = (lin % per_qb) % pairs;
-  const int b = (lin % per_qb) / pairs;
+  const int n_blocks = lc.q_blocks * pairs * lc.n_seqs;
+  int lin = blockIdx.x, split = 0, n_splits = 1, per_split = 0x7fffffff;
+  if (lc.split) {
+    C8Division* d = reinterpret_cast<C8Division*>(smem);   // (before the tiles)
+    if (warp == 0) c8_divide(c, lc, pairs, n_blocks, gridDim.x, d);
+    __syncthreads();
+    if (blockIdx.x == 0)
+      for (int i = threadIdx.x; i <= n_blocks; i += CF::kThreads) a.division[i] = d->first[i];
+    if (int(blockIdx.x) >= d->first[n_blocks]) return;
+    int lo = 0, hi = n_blocks - 1;                         // the last block whose first CTA is not behind this one
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (d->first[mid] <= int(blockIdx.x)) lo = mid; else hi = mid - 1;
+    }
+    lin = lo;
+    split = int(blockIdx.x) - d->first[lo];
+    n_splits = d->first[lo + 1] - d->first[lo];
+    per_split = d->per;
+    __syncthreads();
+  }
+  int b, pair, q0;
+  c8_block_of(c, lc, pairs, lin, b, pair, q0);
   const int head0 = pair * n_tiles_q;
   const int kvh = head0 / (c.n_q / c.n_kv);
-  const int q_len = c.q_lens ? c.q_lens[b] : 1;
+  const int q_len = c.q_lens[b];
   const int ctx = c.context_lens[b];
-  const int q0 = qb * kC8Rows;
   const bool bad = q_len < 0 || q_len > c.max_q_len || ctx < 0 || (long long)ctx + q_len > c.max_len;
-  if (!bad && q0 >= q_len) return;
-  const int start = c.q_lens ? c8_block_prefix(c.q_lens, b, red) : b;
+  if (!bad && (q0 >= q_len || q_len < lc.min_q || q_len >= lc.end_q)) return;
+  const int start = c8_block_prefix(c.q_lens, b, red);
   if (bad || (long long)start + q_len > c.n_tokens) {     // lengths that disagree with what the host was told
     if (threadIdx.x == 0) atomicExch(c.status, kStatusBounds);
     return;
@@ -114,25 +199,24 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   const int rows_here = min(kC8Rows, q_len - q0);
   const int kv_len = ctx + q0 + rows_here;
   const int all_steps = (kv_len + kC8Keys - 1) / kC8Keys;
-  const int per_split = (all_steps + n_splits - 1) / n_splits;
-  const int step0 = split * per_split;
+  const int step0 = split ? split * per_split : 0;
   const int n_steps = min(all_steps - step0, per_split);
-  if (n_steps <= 0) return;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kC8Raw; ++s) { mbar_init(&raw_full[s], 1); mbar_init(&raw_empty[s], 4); }
     for (int s = 0; s < kC8Ring; ++s) {
-      mbar_init(&k_full[s], 4); mbar_init(&k_empty[s], n_tiles_q);
-      mbar_init(&v_full[s], 4); mbar_init(&v_empty[s], n_tiles_q);
+      mbar_init(&k_full[s], CF::kFullCount); mbar_init(&k_empty[s], n_tiles_q);
+      mbar_init(&v_full[s], CF::kFullCount); mbar_init(&v_empty[s], n_tiles_q);
     }
     for (int t = 0; t < 2; ++t) {
-      mbar_init(&q_full[t], 8);
+      mbar_init(&q_full[t], EXPANDED ? 1 : 8);
       mbar_init(&s_full[t], 2); mbar_init(&s_free[t], 4); mbar_init(&p_ready[t], 4);
       mbar_init(&o_full[2 * t], 1); mbar_init(&o_full[2 * t + 1], 1);
       mbar_init(&o_done[t], 1);
       for (int q = 0; q < 4; ++q) mbar_init(&hand[4 * t + q], 1);
     }
     mbar_fence_init();
+    if (EXPANDED) tma_prefetch_desc(&tmQ);
     tma_prefetch_desc(&tmK); tma_prefetch_desc(&tmV);
   }
   if (warp == 1) { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
@@ -144,23 +228,62 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   const uint32_t q_u32 = smem_u32(smem + L::kQOff), k_u32 = smem_u32(smem + L::kKOff), v_u32 = smem_u32(smem + L::kVOff);
 
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kC8RegsLow));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CF::kRegsLow));
     if (warp == 0) {
       // ---------------------------------------------------------------- TMA producer
       if (elect_one()) {
         bool ok = true;
-        for (int j = 0; j < n_steps && ok; ++j) {
-          const int s = j % kC8Raw;
-          if (!mbar_wait(&raw_empty[s], ((j / kC8Raw) & 1) ^ 1)) { ok = false; break; }
-          int page = c.block_table[size_t(b) * c.max_pages_per_seq + step0 + j];
-          if (page < 0 || page >= c.num_pages) { atomicExch(c.status, kStatusBounds); page = 0; }
-          const int ph = page * c.n_kv + kvh;
-          const float sk = c.k_scales[ph], sv = c.v_scales[ph];
-          scales[j % kC8Scales] = make_float4(sk, c8_is_nan(sv) ? sv : float(c8_scale_exp(sv)), 1.f / sv, 0.f);
-          uint8_t* dst = smem + L::kRawOff + s * 2 * L::kRawTile;
-          mbar_expect_tx(&raw_full[s], 2 * L::kRawTile);
-          tma_load_2d(dst, &tmK, &raw_full[s], 0, ph * kC8Keys);
-          tma_load_2d(dst + L::kRawTile, &tmV, &raw_full[s], 0, ph * kC8Keys);
+        if constexpr (EXPANDED) {
+          for (int t = 0; t < n_tiles_q; ++t) {
+            mbar_expect_tx(&q_full[t], L::kQTile);
+            for (int h = 0; h < DH / 64; ++h)
+              tma_load_3d(smem + L::kQOff + t * L::kQTile + h * (kC8Rows * 128), &tmQ, &q_full[t], h * 64, head0 + t, tok0);
+          }
+          const size_t place0 = (size_t(b - lc.seq0) * lc.ws_pages + step0) * c.n_kv + kvh;
+          float4 sc = lc.ws_scales[place0];
+          for (int j = 0; j < n_steps && ok; ++j) {
+            const int r = j % kC8Ring;
+            const uint32_t ph = ((j / kC8Ring) & 1) ^ 1;
+            const size_t place = place0 + size_t(j) * c.n_kv;                // this page's tiles in the workspace
+            const float4 next = j + 1 < n_steps ? lc.ws_scales[place + c.n_kv] : sc;
+            if (!mbar_wait(&k_empty[r], ph)) { ok = false; break; }
+            scales[j % kC8Scales] = sc;
+            mbar_expect_tx(&k_full[r], L::kTile);
+#pragma unroll
+            for (int h = 0; h < DH / 64; ++h) tma_load_2d(smem + L::kKOff + r * L::kTile + h * (kC8Keys * 128), &tmK, &k_full[r], h * 64, int(place) * kC8Keys);
+            if (!mbar_wait(&v_empty[r], ph)) { ok = false; break; }
+            mbar_expect_tx(&v_full[r], L::kTile);
+#pragma unroll
+            for (int h = 0; h < DH / 64; ++h) tma_load_2d(smem + L::kVOff + r * L::kTile + h * (kC8Keys * 128), &tmV, &v_full[r], h * 64, int(place) * kC8Keys);
+            sc = next;
+          }
+        } else {
+          // (the page id of the step after the next and the scales of the next are loaded while this one's stage is waited for)
+          const int* ids = c.block_table + size_t(b) * c.max_pages_per_seq + step0;
+          auto place = [&](int page) {
+            if (page < 0 || page >= c.num_pages) { atomicExch(c.status, kStatusBounds); page = 0; }
+            return page * c.n_kv + kvh;
+          };
+          int ph = place(ids[0]), page_next = n_steps > 1 ? ids[1] : 0;
+          float sk = c.k_scales[ph], sv = c.v_scales[ph];
+          for (int j = 0; j < n_steps && ok; ++j) {
+            const int s = j % kC8Raw;
+            int ph_next = 0;
+            float sk_next = 0.f, sv_next = 1.f;
+            if (j + 1 < n_steps) {
+              ph_next = place(page_next);
+              sk_next = c.k_scales[ph_next];
+              sv_next = c.v_scales[ph_next];
+            }
+            if (j + 2 < n_steps) page_next = ids[j + 2];
+            if (!mbar_wait(&raw_empty[s], ((j / kC8Raw) & 1) ^ 1)) { ok = false; break; }
+            scales[j % kC8Scales] = make_float4(sk, c8_is_nan(sv) ? sv : float(c8_scale_exp(sv)), 1.f / sv, 0.f);
+            uint8_t* dst = smem + L::kRawOff + s * 2 * L::kRawTile;
+            mbar_expect_tx(&raw_full[s], 2 * L::kRawTile);
+            tma_load_2d(dst, &tmK, &raw_full[s], 0, ph * kC8Keys);
+            tma_load_2d(dst + L::kRawTile, &tmV, &raw_full[s], 0, ph * kC8Keys);
+            ph = ph_next; sk = sk_next; sv = sv_next;
+          }
         }
         if (!ok) atomicExch(c.status, kStatusTimeout);
       }
@@ -168,7 +291,7 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
       // ---------------------------------------------------------------- MMA issuers, one per tile
       const int t = warp - 1;
       if (t < n_tiles_q && elect_one()) {
-        constexpr uint32_t idesc_s = umma_idesc_f16(kC8Rows, kC8Keys);
+        constexpr uint32_t idesc_s = EXPANDED ? umma_idesc_bf16(kC8Rows, kC8Keys) : umma_idesc_f16(kC8Rows, kC8Keys);
         constexpr uint32_t idesc_o = umma_idesc_f16(kC8Rows, DH) | (1u << 16);       // B operand (V) is MN-major
         bool ok = mbar_wait(&q_full[t], 0);
         int q = 0, p = 0;                                                 // next Q K^T, next P V
@@ -213,8 +336,9 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
         if (!ok) atomicExch(c.status, kStatusTimeout);
       }
     }
-  } else if (warp < kC8SoftWarp) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kC8RegsConv));
+  } else if (warp < CF::kSoftWarp) {
+    if constexpr (!EXPANDED) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CF::kRegsConv));
     // ------------------------------------------------------------------ converters: codes -> fp16 operand tiles
     // A thread takes 16 codes of a row at a time; its 32 bytes of fp16 go to two 16-byte chunks of the row's 128-byte
     // line in the 64-column half they belong to.  Lanes of the upper half write their chunks in the other order, so that
@@ -223,7 +347,7 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
     constexpr int CH = DH / 16;
     bool ok = true;
     auto convert = [&](const uint8_t* src, uint8_t* dst, int valid_rows) {
-#pragma unroll 2
+#pragma unroll 4
       for (int p = tid; p < kC8Keys * CH; p += 128) {
         const int row = p / CH, ch = p % CH;
         uint4 x = *reinterpret_cast<const uint4*>(src + row * 128 + (((ch ^ row) & 7) << 4));
@@ -256,10 +380,11 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
       if (lane == 0) { mbar_arrive(&v_full[r]); mbar_arrive(&raw_empty[s]); }
     }
     if (!ok && lane == 0) atomicExch(c.status, kStatusTimeout);
+    }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kC8RegsHigh));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(CF::kRegsHigh));
     // ------------------------------------------------------------------ softmax, two threads per query row
-    const int grp = (warp - kC8SoftWarp) >> 2;               // four consecutive warps cover the four lane quarters
+    const int grp = (warp - CF::kSoftWarp) >> 2;               // four consecutive warps cover the four lane quarters
     const int t = grp >> 1;                                  // tile of this warp group
     const int g = grp & 1;                                   // this thread takes the steps j with j % 2 == g
     if (t < n_tiles_q) {
@@ -275,9 +400,9 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
       float* m_hand = reinterpret_cast<float*>(smem + L::kHandOff) + (t * kC8Rows + row) * 2;
       uint64_t* hand_bar = &hand[4 * t + quarter];
 
-      // ---- the row of Q: each of its two threads takes half of the columns
-      float rf;                                              // log2-domain factor of the row's scores
-      {
+      float rf = a.scale_log2;                               // log2-domain factor of the row's scores
+      if constexpr (!EXPANDED) {
+        // ---- the row of Q: each of its two threads takes half of the columns
         constexpr int QC = DH / 16;                          // 8-element chunks of a thread
         uint4 v[QC];
         uint32_t mx = 0;
@@ -387,7 +512,7 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
         // probabilities, written as the fp16 A operand of the PV product (exp2(-inf) = 0 handles the mask)
         const uint32_t p_addr = p_base + (j & 1) * 32;
         if (j >= 2 && !mbar_wait(&o_full[2 * t + ph], ((j - 2) >> 1) & 1)) { ok = false; break; }   // P V of step j-2 has read this buffer
-        uint64_t rs2[4] = {0ull, 0ull, 0ull, 0ull};           // four independent chains of (even, odd) partial sums
+        uint64_t rs2[2] = {0ull, 0ull};                       // two independent chains of (even, odd) partial sums
         const uint64_t sc2 = pack_f32x2(sc, sc), of2 = pack_f32x2(off, off);
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {
@@ -404,15 +529,14 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
           uint32_t pk[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            rs2[i & 3] = add_f32x2(rs2[i & 3], pack_f32x2(e[2 * i], e[2 * i + 1]));
+            rs2[i & 1] = add_f32x2(rs2[i & 1], pack_f32x2(e[2 * i], e[2 * i + 1]));
             pk[i] = pack_f16(e[2 * i], e[2 * i + 1]);
           }
           tmem_st8(p_addr + q4 * 8, pk);
         }
-        float rs4[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) { float lo, hi; unpack_f32x2(rs2[q], lo, hi); rs4[q] = lo + hi; }
-        l_run = fmaf((rs4[0] + rs4[1]) + (rs4[2] + rs4[3]), sc4.z, l_run);
+        float sum0, sum1;
+        unpack_f32x2(add_f32x2(rs2[0], rs2[1]), sum0, sum1);
+        l_run = fmaf(sum0 + sum1, sc4.z, l_run);
         if (!o_seen && !mbar_wait(&o_full[2 * t + (ph ^ 1)], ((j - 1) >> 1) & 1)) { ok = false; break; }
         tmem_st_wait();                                      // P is in tensor memory
         tc_fence_before();
@@ -516,7 +640,7 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
 constexpr int kC8JoinThreads = 256;
 template <int DH>
 __global__ void __launch_bounds__(kC8JoinThreads)
-cache8_join_kernel(const Cache8AttendArgs a, const int q_blocks, const int n_splits) {
+cache8_join_kernel(const Cache8AttendArgs a, const C8Launch lc) {
   pdl_wait();
   pdl_launch_dependents();
   __shared__ int red[kC8JoinThreads / 32];
@@ -525,23 +649,17 @@ cache8_join_kernel(const Cache8AttendArgs a, const int q_blocks, const int n_spl
   const int n_tiles_q = c8_heads_per_block(c);
   const int pairs = c.n_q / n_tiles_q;
   const int lin = blockIdx.x, t = blockIdx.y;
-  const int per_qb = pairs * c.n_seqs;
-  const int qb = q_blocks - 1 - lin / per_qb;
-  const int pair = (lin % per_qb) % pairs;
-  const int b = (lin % per_qb) / pairs;
+  const int first = a.division[lin], used = a.division[lin + 1] - first;
+  if (used < 2) return;                                    // (one CTA: it has written the output itself)
+  int b, pair, q0;
+  c8_block_of(c, lc, pairs, lin, b, pair, q0);
   const int head = pair * n_tiles_q + t;
-  const int q_len = c.q_lens ? c.q_lens[b] : 1;
-  const int ctx = c.context_lens[b];
-  const int q0 = qb * kC8Rows;
-  if (q_len < 0 || q_len > c.max_q_len || ctx < 0 || (long long)ctx + q_len > c.max_len || q0 >= q_len) return;
-  const int start = c.q_lens ? c8_block_prefix(c.q_lens, b, red) : b;
+  const int q_len = c.q_lens[b];
+  const int start = c8_block_prefix(c.q_lens, b, red);
   if ((long long)start + q_len > c.n_tokens) return;
   const int rows_here = min(kC8Rows, q_len - q0);
-  const int all_steps = (ctx + q0 + rows_here + kC8Keys - 1) / kC8Keys;
-  const int per_split = (all_steps + n_splits - 1) / n_splits;
-  const int used = (all_steps + per_split - 1) / per_split;
   for (int row = blockIdx.z * (kC8JoinThreads / 32) + warp; row < rows_here; row += gridDim.z * (kC8JoinThreads / 32)) {
-    auto prow = [&](int s) { return ((size_t(lin) * n_splits + s) * 2 + t) * kC8Rows + row; };
+    auto prow = [&](int s) { return (size_t(first + s) * 2 + t) * kC8Rows + row; };
     float m = -INFINITY;
     for (int s = lane; s < used; s += 32) m = fmaxf(m, a.part_ml[prow(s) * 2]);
 #pragma unroll
@@ -549,12 +667,24 @@ cache8_join_kernel(const Cache8AttendArgs a, const int q_blocks, const int n_spl
     float acc[DH / 32], l = 0.f;
 #pragma unroll
     for (int q = 0; q < DH / 32; ++q) acc[q] = 0.f;
-    for (int s = 0; s < used; ++s) {
-      const float ms = a.part_ml[prow(s) * 2], ls = a.part_ml[prow(s) * 2 + 1];
-      const float f = ms == m ? 1.f : (ms == -INFINITY ? 0.f : fast_exp2(ms - m));
-      l += f * ls;
+    for (int s0 = 0; s0 < used; s0 += 4) {                 // four splits' loads in flight
+      float ms[4], ls[4], v[4][DH / 32];
 #pragma unroll
-      for (int q = 0; q < DH / 32; ++q) acc[q] += f * a.part_o[prow(s) * DH + q * 32 + lane];
+      for (int u = 0; u < 4; ++u) {
+        const size_t p = prow(min(s0 + u, used - 1));
+        ms[u] = a.part_ml[p * 2];
+        ls[u] = a.part_ml[p * 2 + 1];
+#pragma unroll
+        for (int q = 0; q < DH / 32; ++q) v[u][q] = a.part_o[p * DH + q * 32 + lane];
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (s0 + u >= used) break;
+        const float f = ms[u] == m ? 1.f : (ms[u] == -INFINITY ? 0.f : fast_exp2(ms[u] - m));
+        l += f * ls[u];
+#pragma unroll
+        for (int q = 0; q < DH / 32; ++q) acc[q] += f * v[u][q];
+      }
     }
     const float inv = 1.f / l;
     __nv_bfloat16* dst = a.out + (long long)(start + q0 + row) * a.out_stride + head * c.dh;
@@ -565,52 +695,144 @@ cache8_join_kernel(const Cache8AttendArgs a, const int q_blocks, const int n_spl
   }
 }
 
+// Codes of the pages of sequences [seq0, seq0 + n) -> operand tiles [sequence][page][n_kv][64][DH] (exact, unscaled; a
+// 96-wide head zero-padded) and their scales.  K becomes bf16, the type of the queries it meets, V fp16, the type of P.  One block per (page, KV head, K or V); rows behind the sequence's last
+// token become zeros.
+constexpr int kC8ExpThreads = 128;
 template <int FMT, int DH>
+__global__ void __launch_bounds__(kC8ExpThreads)
+cache8_expand_kernel(const Cache8Args c, const C8Launch lc, __nv_bfloat16* k_ws, __half* v_ws, float4* ws_scales) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int page_i = blockIdx.x, kvh = blockIdx.y >> 1, b = lc.seq0 + blockIdx.z;
+  const bool is_v = blockIdx.y & 1;
+  const int q_len = c.q_lens[b], ctx = c.context_lens[b];
+  if (q_len < lc.min_q || q_len > c.max_q_len || ctx < 0 || (long long)ctx + q_len > c.max_len) return;
+  const int rows = min(ctx + q_len - page_i * kC8Keys, kC8Keys);
+  if (rows <= 0) return;
+  int page = c.block_table[size_t(b) * c.max_pages_per_seq + page_i];
+  if (page < 0 || page >= c.num_pages) { if (threadIdx.x == 0) atomicExch(c.status, kStatusBounds); page = 0; }
+  const size_t ph = size_t(page) * c.n_kv + kvh;
+  const size_t place = (size_t(blockIdx.z) * lc.ws_pages + page_i) * c.n_kv + kvh;
+  if (!is_v && threadIdx.x == 0) {
+    const float sv = c.v_scales[ph];
+    ws_scales[place] = make_float4(c.k_scales[ph], c8_is_nan(sv) ? sv : float(c8_scale_exp(sv)), 1.f / sv, 0.f);
+  }
+  const uint8_t* src = (is_v ? c.v_pages : c.k_pages) + ph * kC8Keys * c.dh;
+  uint4* dst = reinterpret_cast<uint4*>(is_v ? static_cast<void*>(v_ws + place * kC8Keys * DH) : static_cast<void*>(k_ws + place * kC8Keys * DH));
+  constexpr int CH = DH / 8, PER = kC8Keys * CH / kC8ExpThreads;         // 8-code pieces of a row, of a thread
+  uint2 x[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int p = i * kC8ExpThreads + threadIdx.x, row = p / CH, ch = p % CH;
+    x[i] = make_uint2(0, 0);
+    if (row < rows && ch * 8 < c.dh) x[i] = *reinterpret_cast<const uint2*>(src + row * c.dh + ch * 8);
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    uint4 o;
+    if (is_v) {
+      c8_decode_natural<FMT>(x[i].x, o.x, o.y);
+      c8_decode_natural<FMT>(x[i].y, o.z, o.w);
+    } else {
+      float v[4], u[4];
+      c8_decode4<FMT>(x[i].x, v);
+      c8_decode4<FMT>(x[i].y, u);
+      o = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(u[0], u[1]), pack_bf16(u[2], u[3]));
+    }
+    dst[i * kC8ExpThreads + threadIdx.x] = o;
+  }
+}
+
+template <int FMT, int DH, bool EXPANDED>
 static cudaError_t configure_t() {
   cudaFuncAttributes fa;
-  cudaError_t e = cudaFuncGetAttributes(&fa, cache8_chunk_kernel<FMT, DH>);
+  cudaError_t e = cudaFuncGetAttributes(&fa, cache8_chunk_kernel<FMT, DH, EXPANDED>);
   if (e != cudaSuccess) return e;
   // the register hand-over inside the kernel assumes this many at launch; anything else is refused here
-  if (fa.numRegs != kC8RegsLaunch) return cudaErrorInvalidConfiguration;
-  return cudaFuncSetAttribute(cache8_chunk_kernel<FMT, DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(C8Smem<DH>::kBytes));
+  if (fa.numRegs != C8Cfg<EXPANDED>::kRegsLaunch) return cudaErrorInvalidConfiguration;
+  return cudaFuncSetAttribute(cache8_chunk_kernel<FMT, DH, EXPANDED>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(C8Smem<DH, EXPANDED>::kBytes));
 }
 
 cudaError_t cache8_chunk_configure() {
-  cudaError_t e = configure_t<kC8E4M3, 64>();
-  if (e == cudaSuccess) e = configure_t<kC8E4M3, 128>();
-  if (e == cudaSuccess) e = configure_t<kC8Int8, 64>();
-  if (e == cudaSuccess) e = configure_t<kC8Int8, 128>();
+  cudaError_t e = configure_t<kC8E4M3, 64, false>();
+  if (e == cudaSuccess) e = configure_t<kC8E4M3, 128, false>();
+  if (e == cudaSuccess) e = configure_t<kC8Int8, 64, false>();
+  if (e == cudaSuccess) e = configure_t<kC8Int8, 128, false>();
+  if (e == cudaSuccess) e = configure_t<kC8E4M3, 64, true>();        // (the same code for both formats)
+  if (e == cudaSuccess) e = configure_t<kC8E4M3, 128, true>();
   return e;
 }
 
+int cache8_chunk_division_ints() { return kC8MaxSplitBlocks + 1; }
 size_t cache8_chunk_part_rows(int n_sms) { return size_t(n_sms) * 2 * kC8Rows; }
 
+// A call whose longest chunk has at least this many query rows per KV head (tokens x query heads of the head) expands its
+// sequences' pages once instead of converting them in every block that reads them.  Expanding costs about 5 bytes per code
+// at the memory's rate (0.015 us a page and head of 128 wide, 0.0075 of 64); a block of 256 rows that converts takes 1.4 us
+// a page where one on expanded tiles takes 1.05, on one of 148 SMs: break-even at 6 blocks a KV head, 3 with narrow heads.
+// Chunks below an eighth of that (single tokens of a mixed batch) keep converting.
+int cache8_expand_min_tokens(int group, int dh) { return ((dh > 64 ? 1536 : 768) + group - 1) / group; }
+
 template <int FMT, int DH>
-static int launch_chunk_t(const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a, int n_sms, cudaStream_t st) {
+static int launch_chunk_t(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a, const Cache8Workspace& ws, int n_sms, cudaStream_t st) {
   const Cache8Args& c = a.c;
-  const int tiles = (c.n_q / c.n_kv) % 2 == 0 ? 2 : 1;
-  const int q_blocks = (c.max_q_len + kC8Rows - 1) / kC8Rows;
-  const long long blocks = (long long)q_blocks * (c.n_q / tiles) * c.n_seqs;
-  // one CTA per SM: a call that fills less than half of them splits its keys, at least 4 pages (and a CTA's start-up and
-  // the joining pass) a split
-  int splits = int(blocks < 1 ? 1 : n_sms / blocks);
-  const int most = (c.max_kv_pages + 3) / 4;
-  if (splits > most) splits = most;
-  if (splits < 1) splits = 1;
-  launch_pdl(cache8_chunk_kernel<FMT, DH>, dim3(unsigned(blocks * splits)), dim3(kC8Threads), size_t(C8Smem<DH>::kBytes), st, tmK, tmV, a, q_blocks, splits);
-  if (splits > 1) {
-    const int z = c.max_q_len < kC8Rows ? (c.max_q_len + 7) / 8 : kC8Rows / 8;
-    launch_pdl(cache8_join_kernel<DH>, dim3(unsigned(blocks), tiles, z), dim3(kC8JoinThreads), 0, st, a, q_blocks, splits);
+  const int G = c.n_q / c.n_kv, tiles = G % 2 == 0 ? 2 : 1;
+  const bool expand = c.max_q_len >= cache8_expand_min_tokens(G, c.dh);
+  const int long_q = (cache8_expand_min_tokens(G, c.dh) + 7) / 8;        // chunks from here on run on expanded tiles, if any
+  // query blocks of a launch over n sequences of up to `longest` tokens; one CTA per SM, so a launch of fewer blocks
+  // than that splits their keys.  Returns the CTAs.
+  auto plan = [&](C8Launch& lc, int longest, int n) {
+    lc.q_blocks = (longest + kC8Rows - 1) / kC8Rows;
+    lc.n_seqs = n;
+    const long long blocks = (long long)lc.q_blocks * (c.n_q / tiles) * n;
+    lc.split = blocks < n_sms && blocks <= kC8MaxSplitBlocks && c.max_kv_pages > kC8MinSteps;
+    return unsigned(lc.split ? n_sms : blocks);
+  };
+  auto join = [&](const C8Launch& lc, int longest) {
+    if (!lc.split) return 0;
+    const int z = ((longest < kC8Rows ? longest : kC8Rows) + 7) / 8;             // a row a warp
+    launch_pdl(cache8_join_kernel<DH>, dim3(unsigned(lc.q_blocks) * (c.n_q / tiles) * lc.n_seqs, tiles, z), dim3(kC8JoinThreads), 0, st, a, lc);
+    return 1;
+  };
+  int n = 0;
+  // ---- short chunks: codes converted by the blocks that read them.  (No sequence has fewer tokens than those that the
+  // others, at max_q_len each, leave over.)
+  const long long least = c.n_tokens - (long long)(c.n_seqs - 1) * c.max_q_len;
+  if (!expand || least < long_q) {
+    C8Launch lc = {};
+    const int longest = expand ? long_q - 1 : c.max_q_len;
+    lc.end_q = longest + 1;
+    if (longest > 0) {
+      const unsigned ctas = plan(lc, longest, c.n_seqs);
+      launch_pdl(cache8_chunk_kernel<FMT, DH, false>, dim3(ctas), dim3(C8Cfg<false>::kThreads), size_t(C8Smem<DH, false>::kBytes), st, tmK, tmK, tmV, a, lc);
+      n += 1 + join(lc, longest);
+    }
   }
-  return splits > 1 ? 2 : 1;
+  if (!expand) return n;
+  // ---- long chunks, as many sequences at a time as the workspace holds
+  int group = int(ws.pages / c.max_kv_pages);
+  if (group > c.n_seqs) group = c.n_seqs;
+  for (int s0 = 0; s0 < c.n_seqs; s0 += group) {
+    C8Launch lc = {};
+    lc.min_q = long_q;
+    lc.end_q = c.max_q_len + 1;
+    lc.ws_pages = c.max_kv_pages;
+    lc.ws_scales = ws.scales;
+    lc.seq0 = s0;
+    const unsigned ctas = plan(lc, c.max_q_len, c.n_seqs - s0 < group ? c.n_seqs - s0 : group);
+    launch_pdl(cache8_expand_kernel<FMT, DH>, dim3(c.max_kv_pages, c.n_kv * 2, lc.n_seqs), dim3(kC8ExpThreads), 0, st, c, lc, ws.k, ws.v, ws.scales);
+    launch_pdl(cache8_chunk_kernel<kC8E4M3, DH, true>, dim3(ctas), dim3(C8Cfg<true>::kThreads), size_t(C8Smem<DH, true>::kBytes), st, tmQ, ws.tmK, ws.tmV, a, lc);
+    n += 2 + join(lc, c.max_q_len);
+  }
+  return n;
 }
 
-int launch_cache8_chunk(int fmt, const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a, int n_sms, cudaStream_t st) {
+int launch_cache8_chunk(int fmt, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a, const Cache8Workspace& ws,
+                        int n_sms, cudaStream_t st) {
   if (a.c.n_seqs <= 0 || a.c.n_tokens <= 0) return 0;
-  if (fmt == kC8E4M3) {
-    return a.c.dh > 64 ? launch_chunk_t<kC8E4M3, 128>(tmK, tmV, a, n_sms, st) : launch_chunk_t<kC8E4M3, 64>(tmK, tmV, a, n_sms, st);
-  }
-  return a.c.dh > 64 ? launch_chunk_t<kC8Int8, 128>(tmK, tmV, a, n_sms, st) : launch_chunk_t<kC8Int8, 64>(tmK, tmV, a, n_sms, st);
+  if (fmt == kC8E4M3) return a.c.dh > 64 ? launch_chunk_t<kC8E4M3, 128>(tmQ, tmK, tmV, a, ws, n_sms, st) : launch_chunk_t<kC8E4M3, 64>(tmQ, tmK, tmV, a, ws, n_sms, st);
+  return a.c.dh > 64 ? launch_chunk_t<kC8Int8, 128>(tmQ, tmK, tmV, a, ws, n_sms, st) : launch_chunk_t<kC8Int8, 64>(tmQ, tmK, tmV, a, ws, n_sms, st);
 }
 
 }  // namespace foe

@@ -10,9 +10,10 @@ struct foe_cache {
   void* memory;                         // the workspace that the pointers below are parts of
   int* status;
   float *part_o, *part_ml, *lse, *logits;
-  int* split_done;
+  int *split_done, *division;
   size_t split_done_count;
   long long logits_stride;
+  foe::Cache8Workspace ws;
   __nv_bfloat16 *k_stage, *v_stage;     // K and V rows of a layer's call, in pages of 64 consecutive tokens
   int *tok_pos, *tok_slot;
   cudaStream_t last_stream;

@@ -285,6 +285,35 @@ def test_attend_chunk_that_fills_the_gpu(n_q, n_kv, dh):
 
 
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("n_q,n_kv,dh", [(4, 2, 128), (3, 1, 96), (4, 4, 64)])
+def test_attend_long_chunks_beside_short_ones(fmt, n_q, n_kv, dh):
+    """Chunks long enough to run on expanded tiles, short ones and single tokens in one call; garbage behind the last
+    rows."""
+    ctx, q = [0, 300, 130, 64, 1000], [600, 1, 512, 511, 0]
+    total = [a + b for a, b in zip(ctx, q)]
+    s = Setup(n_q, n_kv, dh, fmt, total, seed=60)
+    s.fill(total)
+    run_attend(s, ctx, q, scale=1.5, weights=True, window=2)
+
+
+def test_attend_long_chunks_in_groups():
+    """More sequences than the expanded tiles have room for at a time (the workspace keeps 256 MiB)."""
+    n_q, n_kv, dh, n = 8, 8, 128, 18
+    ctx, q = [7400 + 3 * i for i in range(n)], [513 if i in (1, 9, 17) else 2 for i in range(n)]
+    s = Setup(n_q, n_kv, dh, "e4m3", [a + b for a, b in zip(ctx, q)], seed=61, garbage=False)
+    s.fill([a + b for a, b in zip(ctx, q)])
+    x = s.randn(sum(q), n_q, dh, scale=1.5)
+    out = s.ops.attend(x.cuda(), s.view(ctx, q))
+    assert s.ops.poll_status() == 0
+    kp, vp = s.refs()
+    starts = [sum(q[:b]) for b in range(n)]
+    for b, i in ((0, 0), (1, 0), (1, 512), (9, 200), (16, 1), (17, 512)):
+        t = starts[b] + i
+        o, mag, big, _ = ref.attend(kp, vp, s.table[b:b + 1], [ctx[b] + i], [1], x[t:t + 1])
+        ref.check_attend(out[t:t + 1], o, mag, big)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
 @pytest.mark.parametrize("q", [None, [3, 70]])
 def test_attend_sharp_softmax_and_uneven_pages(fmt, q):
     """Scores of hundreds (one key takes all), pages whose scales differ by up to 2^30, queries of extreme size, zero
