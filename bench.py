@@ -661,7 +661,8 @@ def run_serve(args):
     reqs = sv.synthetic_trace(n_req, rate=rate, seed=11)
     num_pages = 4096                                        # 262,144 tokens of KV per layer
     runner = sv.FoeStackRunner(shape, n_layers, seed=2, num_pages=num_pages, max_batch_tokens=max_batch_tokens,
-                               max_seqs=max_seqs, max_context=max_context)
+                               max_seqs=max_seqs, max_context=max_context,
+                               cache_format=None if args.cache == "bf16" else args.cache, kv_budget=args.kv_budget or None)
     # Warm-up: every kernel family the run can launch (large and small prefill chunks, mixed batches, decode steps of
     # several sizes) once, so that no one-time cost of a first launch (module loading, kernel attributes) lands inside
     # an iteration whose device time is charged to the requests waiting on it.  The collector is off during the run for
@@ -670,7 +671,9 @@ def run_serve(args):
     for seed, n, pr, orr in ((12, 3, (512, 4096), (2, 4)), (13, 12, (64, 9000), (2, 12))):
         warm = sv.synthetic_trace(n, rate=1e6, seed=seed, prompt_range=pr, output_range=orr)
         sv.Engine(sv.Scheduler(sv.PagePool(num_pages), max_batch_tokens, max_seqs, chunk), runner.forward).run(warm)
-    eng = sv.Engine(sv.Scheduler(sv.PagePool(num_pages), max_batch_tokens, max_seqs, chunk), runner.forward)
+    pool = sv.PagePool(num_pages)
+    runner.pool = pool
+    eng = sv.Engine(sv.Scheduler(pool, max_batch_tokens, max_seqs, chunk), runner.forward)
     gc.collect()
     gc.disable()
     try:
@@ -684,7 +687,9 @@ def run_serve(args):
                           config=dict(workload=f"{n_layers}-layer stack of the workload-2 layer; {n_req} requests, Poisson "
                                                f"{rate} req/s, prompts log-uniform 1024..16384, outputs 32..256; continuous "
                                                f"batching, <= {max_batch_tokens} tokens and {max_seqs} sequences per iteration, "
-                                               f"prompt chunks of {chunk}"),
+                                               f"prompt chunks of {chunk}"
+                                               + ("" if args.cache == "bf16" else f"; KV cache {args.cache}")
+                                               + (f", cut to {args.kv_budget} tokens after the prompt" if args.kv_budget else "")),
                           requests=len(done), iterations=eng.iterations, busy_seconds=eng.clock,
                           tokens_per_s=toks / eng.clock, mean_batch_tokens=sum(eng.batch_tokens) / max(1, len(eng.batch_tokens)),
                           **rep)))
@@ -792,6 +797,8 @@ def main():
     ap.add_argument("--stack", action="store_true", help="16-layer stack (workload 5): FoE and the one-cluster MoE twin")
     ap.add_argument("--shard", action="store_true", help="one cluster per rank, all ranks emulated on this device: per-rank kernel time")
     ap.add_argument("--serve", action="store_true", help="request-level latency run (continuous batching on a 4-layer stack)")
+    ap.add_argument("--cache", choices=["bf16", "e4m3", "int8"], default="bf16", help="--serve: what K and V are held in")
+    ap.add_argument("--kv-budget", type=int, default=0, help="--serve with an 8-bit cache: tokens a request keeps after its prompt (0: all)")
     ap.add_argument("--requests", type=int, default=48)
     ap.add_argument("--rate", type=float, default=20.0, help="--serve: Poisson arrival rate, requests per second")
     args = ap.parse_args()

@@ -40,6 +40,9 @@ class FoeCacheView(ctypes.Structure):
                [(n, ctypes.c_int) for n in ("n_seqs", "max_pages_per_seq", "num_pages", "n_tokens", "max_q_len")]
 
 
+# the current stream's handle without the Stream object around it, where torch offers that (a microsecond less a call)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+
 _declared = False
 
 
@@ -179,7 +182,7 @@ class CacheOps:
         return w_in.data_ptr(), w_out.data_ptr(), shape[2]
 
     def _stream(self, stream) -> int:
-        return torch.cuda.current_stream(self.index).cuda_stream if stream is None else stream.cuda_stream
+        return _current_stream(self.index) if stream is None else stream.cuda_stream
 
     # ---- the calls
     def append(self, k: torch.Tensor, v: torch.Tensor, view: Paged8, max_q_len: Optional[int] = None, stream=None) -> None:

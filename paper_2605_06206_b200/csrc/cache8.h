@@ -73,6 +73,7 @@ struct Cache8EvictArgs {
 
 // fmt: kC8E4M3 or kC8Int8 (cache8.cuh)
 void launch_cache8_append(int fmt, const Cache8AppendArgs& a, cudaStream_t st);
+// single tokens: q_lens nullptr, or the sequences with q_lens == 1
 void launch_cache8_decode(int fmt, const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a, int n_sms,
                           cudaStream_t st);
 size_t cache8_decode_part_rows(int n_sms);   // rows of part_o / part_ml
@@ -87,9 +88,10 @@ struct Cache8Workspace {
   CUtensorMap tmK, tmV;
 };
 // chunks: q_lens given, n_tokens rows in all; tmQ maps q as [tokens][heads][dh] with boxes of 128 x 1 x 64.  part_o / part_ml hold cache8_chunk_part_rows(n_sms) rows; ws is used by calls
-// with max_q_len >= cache8_expand_min_tokens(n_q / n_kv, dh).  Returns the number of kernels launched.
+// with max_q_len >= cache8_expand_min_tokens(n_q / n_kv, dh).
+// Sequences of fewer than min_q tokens are left out.  Returns the number of kernels launched.
 int launch_cache8_chunk(int fmt, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a,
-                        const Cache8Workspace& ws, int n_sms, cudaStream_t st);
+                        const Cache8Workspace& ws, int min_q, int n_sms, cudaStream_t st);
 int cache8_expand_min_tokens(int group, int dh);    // group: query heads per KV head
 int cache8_chunk_division_ints();
 size_t cache8_chunk_part_rows(int n_sms);

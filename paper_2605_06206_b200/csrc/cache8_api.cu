@@ -128,11 +128,8 @@ foe_status cache8_check(const foe_cache* h, const foe_cache_view* v, bool need_q
     if ((long long)v->n_seqs * ((v->max_q_len + 127) / 128) * h->cfg.n_q_heads >= (1LL << 31)) return FOE_ERR_SHAPE;
     *rows = v->n_tokens;
   }
-  if (!v->q_lens) {
-    const Cache8Args c = cache8_args(h, v, nullptr);
-    // the decode kernel numbers the pages of all (sequence, KV head) pairs with 32-bit integers
-    if ((long long)v->n_seqs * h->cfg.n_kv_heads * c.max_kv_pages >= (1LL << 30)) return FOE_ERR_SHAPE;
-  }
+  // the kernel for single tokens numbers the pages of all (sequence, KV head) pairs with 32-bit integers
+  if ((long long)v->n_seqs * h->cfg.n_kv_heads * (cache8_args(h, v, nullptr).max_kv_pages + 8) >= (1LL << 30)) return FOE_ERR_SHAPE;
   return FOE_OK;
 }
 
@@ -178,7 +175,17 @@ int cache8_attend(foe_cache* h, const foe_cache_view* v, const void* q, long lon
   } else {
     CUtensorMap tmQ = tmK;                       // (only long chunks read their queries through a map)
     if (h->ws.pages && a.c.n_tokens > 0 && !make_query_map(&tmQ, q, a.c.n_tokens, a.c.n_q, a.c.dh, q_stride, q_head_stride)) return -1;
-    n = launch_cache8_chunk(h->cfg.format, tmQ, tmK, tmV, a, h->ws, h->n_sms, st);
+    // Sequences with one new token go the way of single tokens: a tile of 128 query rows would read their cache at a
+    // fraction of the memory's rate.  (No sequence has fewer tokens than those that the others, at max_q_len each, leave.)
+    const bool singles = a.c.n_tokens - (long long)(a.c.n_seqs - 1) * a.c.max_q_len < 2;
+    n = 0;
+    if (singles && a.c.n_tokens > 0) {
+      Cache8AttendArgs one = a;
+      one.logits = nullptr;
+      launch_cache8_decode(h->cfg.format, tmK, tmV, one, h->n_sms, st);
+      n = 1;
+    }
+    if (a.c.max_q_len > 1 || !singles) n += launch_cache8_chunk(h->cfg.format, tmQ, tmK, tmV, a, h->ws, singles ? 2 : 0, h->n_sms, st);
   }
   if (w_out) {
     Cache8WeightsArgs w;

@@ -1,4 +1,4 @@
-// Attention of single new tokens over the 8-bit cache, and the accumulation of attention weights.
+// Attention of single new tokens over the 8-bit cache (in a call of chunks: of its sequences with one new token).
 //
 // Decode reads every code of the cache once: 1 byte per K and V element, so the kernel has half the time per element of
 // a bf16 one and its arithmetic has to be lean.
@@ -97,8 +97,22 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   pdl_wait();
   pdl_launch_dependents();
 
+  // A call with q_lens runs its sequences of one new token here and the others as chunks; their lengths are looked over once.
+  if (c.q_lens && blockIdx.x == 0 && warp == 0) {
+    long long sum = 0;
+    bool bad = false;
+    for (int b = lane; b < c.n_seqs; b += 32) {
+      const int n = c.q_lens[b], ctx = c.context_lens[b];
+      bad = bad || n < 0 || n > c.max_q_len || ctx < 0 || (long long)ctx + n > c.max_len;
+      sum += n;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (__any_sync(0xffffffffu, bad || sum != c.n_tokens) && lane == 0) atomicExch(c.status, kStatusBounds);
+  }
+
   DcWalk w;
-  if (!dc_begin<kD8Gap>(c, kD8MinTiles, w)) return;                // (the same in every warp)
+  if (!dc_begin<kD8Gap, true>(c, kD8MinTiles, w)) return;                // (the same in every warp)
 
   if (warp == CF::kWarps) {
     // ------------------------------------------------------------------ producer
@@ -121,7 +135,7 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       }
       off += q.n;
       if (off == len) {
-        dc_advance<kD8Gap>(c, wn, len);
+        dc_advance<kD8Gap, true>(c, wn, len);
         off = 0;
       }
       return q;
@@ -184,7 +198,7 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   int it = 0, st = 0;                                              // pages so far, their next stage and the parity of its phase
   uint32_t ph = 0;
   // pairs whose keys are split over CTAs: at most the CTA's first and its last; their tickets are taken at the end
-  int pend_b[2], pend_kvh[2], pend_c0[2], pend_n[2], n_pend = 0;
+  int pend_b[2], pend_kvh[2], pend_c0[2], pend_n[2], pend_tok[2], n_pend = 0;
 
   while (w.t < w.t_end) {
     const int len = dc_segment_len(w);
@@ -193,6 +207,13 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     const int c_first = pair_first / w.per;
     const int n_segs = (pair_first + w.np - 1) / w.per - c_first + 1;
     const int seg = int(blockIdx.x) - c_first;
+    int tok = b;                                                   // row of the sequence's token
+    if (c.q_lens) {
+      int before = 0;
+      for (int i = lane; i < b; i += 32) before += max(c.q_lens[i], 0);
+      tok = __reduce_add_sync(0xffffffffu, before);
+    }
+    const bool tok_ok = tok < c.n_tokens;                          // (lengths that do not add up are reported above)
     if (w.page == 0 && kvh == 0 && ctid == 0) {
       const int ctx = c.context_lens[b];
       if (ctx < 0 || ctx >= c.max_len) atomicExch(c.status, kStatusBounds);
@@ -209,8 +230,8 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       for (int hh = 0; hh < NC / 4; ++hh) {
         const int d0 = (t4 + 4 * hh) * 16;
         v[hh][0] = v[hh][1] = make_uint4(0, 0, 0, 0);
-        if (n * 8 + g < G && d0 < c.dh) {
-          const uint4* p = reinterpret_cast<const uint4*>(a.q + (long long)b * a.q_stride + (kvh * G + n * 8 + g) * a.q_head_stride + d0);
+        if (n * 8 + g < G && d0 < c.dh && tok_ok) {
+          const uint4* p = reinterpret_cast<const uint4*>(a.q + (long long)tok * a.q_stride + (kvh * G + n * 8 + g) * a.q_head_stride + d0);
           v[hh][0] = __ldg(p);
           v[hh][1] = __ldg(p + 1);
         }
@@ -417,9 +438,9 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         const int r = q / DH, d = q - r * DH;
         float m, l;
         row_ml(r, m, l);
-        if (d < c.dh)                                              // (a 96-wide head is computed zero-padded to 128)
-          a.out[(long long)b * a.out_stride + (kvh * G + r) * c.dh + d] = __float2bfloat16_rn(mo[r * SM::kPitch + d] / l);
-        if (d == 0 && a.lse) a.lse[size_t(b) * c.n_q + kvh * G + r] = m - kD8Shift + log2f(l);
+        if (d < c.dh && tok_ok)                                    // (a 96-wide head is computed zero-padded to 128)
+          a.out[(long long)tok * a.out_stride + (kvh * G + r) * c.dh + d] = __float2bfloat16_rn(mo[r * SM::kPitch + d] / l);
+        if (d == 0 && a.lse && tok_ok) a.lse[size_t(tok) * c.n_q + kvh * G + r] = m - kD8Shift + log2f(l);
       }
     } else {
       // A segment whose wait ran out writes no partial state but still takes its ticket: the counter of its pair
@@ -435,11 +456,11 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
           a.part_ml[(slot * 16 + r) * 2 + 1] = l;
         }
       }
-      pend_b[n_pend & 1] = b; pend_kvh[n_pend & 1] = kvh; pend_c0[n_pend & 1] = c_first; pend_n[n_pend & 1] = n_segs;
+      pend_b[n_pend & 1] = b; pend_kvh[n_pend & 1] = kvh; pend_c0[n_pend & 1] = c_first; pend_n[n_pend & 1] = n_segs; pend_tok[n_pend & 1] = tok;
       ++n_pend;
     }
     d8_bar<CT>();                                                  // mo and mm are free for the next segment
-    dc_advance<kD8Gap>(c, w, len);
+    dc_advance<kD8Gap, true>(c, w, len);
   }
 
   // ---- tickets of the split pairs, and the merge of those this CTA is the last to finish
@@ -452,7 +473,7 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     }
     d8_bar<CT>();
     for (int q = 0; q < n_pend; ++q) {
-      const int b = pend_b[q], kvh = pend_kvh[q], c_first = pend_c0[q], n_segs = pend_n[q];
+      const int b = pend_b[q], kvh = pend_kvh[q], c_first = pend_c0[q], n_segs = pend_n[q], tok = pend_tok[q];
       if (ticket_s[q] != n_segs - 1) continue;
       if (ctid == 0) a.split_done[b * c.n_kv + kvh] = 0;           // re-armed for the next call
       __threadfence();
@@ -495,11 +516,12 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
           }
         }
         const float inv = 1.f / l;
-        __nv_bfloat16* dst = a.out + (long long)b * a.out_stride + (kvh * G + r) * c.dh;
+        if (tok >= c.n_tokens) continue;
+        __nv_bfloat16* dst = a.out + (long long)tok * a.out_stride + (kvh * G + r) * c.dh;
 #pragma unroll
         for (int i = 0; i < DH / 32; ++i)
           if (i * 32 + lane < c.dh) dst[i * 32 + lane] = __float2bfloat16_rn(acc[i] * inv);
-        if (lane == 0 && a.lse) a.lse[size_t(b) * c.n_q + kvh * G + r] = m - kD8Shift + log2f(l);
+        if (lane == 0 && a.lse) a.lse[size_t(tok) * c.n_q + kvh * G + r] = m - kD8Shift + log2f(l);
       }
     }
   }

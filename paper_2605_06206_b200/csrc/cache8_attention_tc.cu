@@ -775,11 +775,11 @@ size_t cache8_chunk_part_rows(int n_sms) { return size_t(n_sms) * 2 * kC8Rows; }
 int cache8_expand_min_tokens(int group, int dh) { return ((dh > 64 ? 1536 : 768) + group - 1) / group; }
 
 template <int FMT, int DH>
-static int launch_chunk_t(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a, const Cache8Workspace& ws, int n_sms, cudaStream_t st) {
+static int launch_chunk_t(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a, const Cache8Workspace& ws, int min_q, int n_sms, cudaStream_t st) {
   const Cache8Args& c = a.c;
   const int G = c.n_q / c.n_kv, tiles = G % 2 == 0 ? 2 : 1;
   const bool expand = c.max_q_len >= cache8_expand_min_tokens(G, c.dh);
-  const int long_q = (cache8_expand_min_tokens(G, c.dh) + 7) / 8;        // chunks from here on run on expanded tiles, if any
+  const int long_q = (cache8_expand_min_tokens(G, c.dh) + 7) / 8;        // chunks from here on run on expanded tiles, if any (at least 6)
   // query blocks of a launch over n sequences of up to `longest` tokens; one CTA per SM, so a launch of fewer blocks
   // than that splits their keys.  Returns the CTAs.
   auto plan = [&](C8Launch& lc, int longest, int n) {
@@ -802,8 +802,9 @@ static int launch_chunk_t(const CUtensorMap& tmQ, const CUtensorMap& tmK, const 
   if (!expand || least < long_q) {
     C8Launch lc = {};
     const int longest = expand ? long_q - 1 : c.max_q_len;
+    lc.min_q = min_q;
     lc.end_q = longest + 1;
-    if (longest > 0) {
+    if (longest >= min_q) {
       const unsigned ctas = plan(lc, longest, c.n_seqs);
       launch_pdl(cache8_chunk_kernel<FMT, DH, false>, dim3(ctas), dim3(C8Cfg<false>::kThreads), size_t(C8Smem<DH, false>::kBytes), st, tmK, tmK, tmV, a, lc);
       n += 1 + join(lc, longest);
@@ -829,10 +830,10 @@ static int launch_chunk_t(const CUtensorMap& tmQ, const CUtensorMap& tmK, const 
 }
 
 int launch_cache8_chunk(int fmt, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a, const Cache8Workspace& ws,
-                        int n_sms, cudaStream_t st) {
+                        int min_q, int n_sms, cudaStream_t st) {
   if (a.c.n_seqs <= 0 || a.c.n_tokens <= 0) return 0;
-  if (fmt == kC8E4M3) return a.c.dh > 64 ? launch_chunk_t<kC8E4M3, 128>(tmQ, tmK, tmV, a, ws, n_sms, st) : launch_chunk_t<kC8E4M3, 64>(tmQ, tmK, tmV, a, ws, n_sms, st);
-  return a.c.dh > 64 ? launch_chunk_t<kC8Int8, 128>(tmQ, tmK, tmV, a, ws, n_sms, st) : launch_chunk_t<kC8Int8, 64>(tmQ, tmK, tmV, a, ws, n_sms, st);
+  if (fmt == kC8E4M3) return a.c.dh > 64 ? launch_chunk_t<kC8E4M3, 128>(tmQ, tmK, tmV, a, ws, min_q, n_sms, st) : launch_chunk_t<kC8E4M3, 64>(tmQ, tmK, tmV, a, ws, min_q, n_sms, st);
+  return a.c.dh > 64 ? launch_chunk_t<kC8Int8, 128>(tmQ, tmK, tmV, a, ws, min_q, n_sms, st) : launch_chunk_t<kC8Int8, 64>(tmQ, tmK, tmV, a, ws, min_q, n_sms, st);
 }
 
 }  // namespace foe

@@ -2,7 +2,8 @@
 // pairs form one list (sequence-major, then KV head, then page) of T entries and CTA c takes the entries
 // [c * per, (c + 1) * per), per = max(min_tiles, ceil(T / grid)).  GAP: entries without a page in front of every pair,
 // which stand for the time that starting a pair costs, so that a CTA whose range holds more pairs gets fewer pages.
-// Args: context_lens, n_seqs, n_kv, max_kv_pages.
+// SINGLES: where the call gives q_lens, only the sequences with one new token count (the others have no entries).
+// Args: context_lens, n_seqs, n_kv, max_kv_pages (SINGLES: q_lens, or nullptr).
 #pragma once
 
 #include "common.cuh"
@@ -18,21 +19,24 @@ struct DcWalk {
   int per;
 };
 
-template <typename Args>
+template <bool SINGLES = false, typename Args>
 __device__ __forceinline__ int dc_pages(const Args& a, int b, int* kv_len) {
+  if constexpr (SINGLES) {
+    if (a.q_lens && a.q_lens[b] != 1) { *kv_len = 0; return 0; }
+  }
   const int ctx = min(max(a.context_lens[b], 0), a.max_kv_pages * 64 - 1);   // (out-of-range values are reported by the QKV step)
   *kv_len = ctx + 1;                                                          // cached tokens + the new one
   return (ctx + 64) >> 6;
 }
 
 // Every warp works this out for itself (all 32 lanes): the CTA's range and where it starts.  False: nothing to do.
-template <int GAP = 0, typename Args>
+template <int GAP = 0, bool SINGLES = false, typename Args>
 __device__ __forceinline__ bool dc_begin(const Args& a, int min_tiles, DcWalk& w) {
   const int lane = threadIdx.x & 31;
   int sum = 0, np_first = 0, kl_first = 0;        // (the first 32 sequences' values are kept for the search below)
   for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
     int kl = 0;
-    const int np = b0 + lane < a.n_seqs ? dc_pages(a, b0 + lane, &kl) : 0;
+    const int np = b0 + lane < a.n_seqs ? dc_pages<SINGLES>(a, b0 + lane, &kl) : 0;
     if (b0 == 0) { np_first = np; kl_first = kl; }
     sum += np + (np > 0 ? GAP : 0);
   }
@@ -47,7 +51,7 @@ __device__ __forceinline__ bool dc_begin(const Args& a, int min_tiles, DcWalk& w
   int base = 0;                                  // entries (per KV head) of the sequences before this chunk of 32
   for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
     int kl = kl_first;
-    const int np = b0 == 0 ? np_first : (b0 + lane < a.n_seqs ? dc_pages(a, b0 + lane, &kl) : 0);
+    const int np = b0 == 0 ? np_first : (b0 + lane < a.n_seqs ? dc_pages<SINGLES>(a, b0 + lane, &kl) : 0);
     const int size = np + (np > 0 ? GAP : 0);
     int incl = size;
 #pragma unroll
@@ -85,7 +89,7 @@ __device__ __forceinline__ int dc_segment_len(const DcWalk& w) { return min(w.np
 template <int GAP = 0>
 __device__ __forceinline__ int dc_pair_first(const DcWalk& w) { return w.seq_first + w.kvh * (w.np + GAP) + GAP; }
 
-template <int GAP = 0, typename Args>
+template <int GAP = 0, bool SINGLES = false, typename Args>
 __device__ __forceinline__ void dc_advance(const Args& a, DcWalk& w, int len) {
   w.t += len;
   w.page += len;
@@ -97,7 +101,11 @@ __device__ __forceinline__ void dc_advance(const Args& a, DcWalk& w, int len) {
       w.kvh = 0;
       w.seq_first += a.n_kv * (w.np + GAP);
       w.b += 1;
-      if (w.t < w.t_end) w.np = dc_pages(a, w.b, &w.kv_len);
+      if (w.t < w.t_end) {
+        w.np = dc_pages<SINGLES>(a, w.b, &w.kv_len);
+        if constexpr (SINGLES)
+          while (w.np == 0 && w.b + 1 < a.n_seqs) w.np = dc_pages<SINGLES>(a, ++w.b, &w.kv_len);
+      }
     }
   }
 }

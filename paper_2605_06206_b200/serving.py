@@ -54,7 +54,8 @@ class Request:
     output_len: int                 # tokens generated after the prompt (>= 1)
     # filled in by the engine
     pages: List[int] = dataclasses.field(default_factory=list)
-    cached: int = 0                 # tokens of this request whose K/V are in the cache
+    cached: int = 0                 # tokens of this request that have been computed
+    dropped: int = 0                # of those, tokens whose K/V an eviction has removed from the cache
     generated: int = 0
     token_times: List[float] = dataclasses.field(default_factory=list)   # clock at which each output token appeared
     finished: Optional[float] = None
@@ -66,6 +67,11 @@ class Request:
     @property
     def prefilling(self) -> bool:
         return self.cached < self.prompt_len
+
+    @property
+    def held(self) -> int:
+        """Tokens whose K/V are in the cache."""
+        return self.cached - self.dropped
 
 
 def poisson_requests(n: int, rate: float, prompt_lens: Sequence[int], output_lens: Sequence[int], u01: Sequence[float]
@@ -213,12 +219,23 @@ class FoeStackRunner:
     """forward() for Engine on a stack of FoE layers (first, middle..., last) with per-layer page pools.
 
     One batch = one foe_prefill per layer (foe_decode when every sequence contributes a single token): sequences in scheduler order, their new tokens concatenated; the
-    block table row of a sequence lists the pages reserved for the request."""
+    block table row of a sequence lists the pages reserved for the request.
+
+    cache_format "e4m3" or "int8" keeps K and V in 8 bits (foe_cache_block in place of foe_prefill / foe_decode): half the
+    bytes per page, so twice the pages in the same memory.  With kv_budget (a number of tokens) a request whose prompt has
+    just been computed is cut to that many tokens in every layer and KV head: the first `sink`, the last `recent`, and those
+    that the last `window` queries of the prompt gave the most weight.  The cut moves them into fresh pages of `pool` and
+    gives back what the rest of the request does not need; when the pool has no room for the move the request stays whole."""
 
     def __init__(self, base_shape, n_layers: int, seed: int, num_pages: int, max_batch_tokens: int, max_seqs: int,
-                 max_context: int, device: str = "cuda"):
+                 max_context: int, device: str = "cuda", cache_format: Optional[str] = None, kv_budget: Optional[int] = None,
+                 sink: int = 4, recent: int = 64, window: int = 32):
         import torch
-        from . import binding, synth
+        from . import binding, cache8, synth
+        assert kv_budget is None or cache_format is not None, "the cut is an operator of the 8-bit cache"
+        self.cache_format, self.kv_budget, self.sink, self.recent, self.window = cache_format, kv_budget, sink, recent, window
+        self.pool: Optional[PagePool] = None                # the scheduler's pool, for the cut
+        self.cuts = 0
         self.torch, self.synth = torch, synth
         self.shape, self.seed, self.device = base_shape, seed, device
         self.max_pages_per_seq = pages_for(max_context)
@@ -233,8 +250,14 @@ class FoeStackRunner:
             del W
         torch.cuda.empty_cache()
         nkv, dh = base_shape.n_kv_heads, base_shape.head_dim
-        self.k = [torch.zeros((num_pages, nkv, PAGE, dh), dtype=torch.bfloat16, device=device) for _ in range(n_layers)]
-        self.v = [torch.zeros((num_pages, nkv, PAGE, dh), dtype=torch.bfloat16, device=device) for _ in range(n_layers)]
+        if cache_format is None:
+            self.k = [torch.zeros((num_pages, nkv, PAGE, dh), dtype=torch.bfloat16, device=device) for _ in range(n_layers)]
+            self.v = [torch.zeros((num_pages, nkv, PAGE, dh), dtype=torch.bfloat16, device=device) for _ in range(n_layers)]
+        else:
+            self.caches = [cache8.empty_cache(base_shape, num_pages, device) for _ in range(n_layers)]
+            # one workspace for all layers: they run one after the other
+            self.ops = cache8.CacheOps(base_shape, cache_format, max_batch_tokens, max_seqs, max_context,
+                                       weights=kv_budget is not None, layers=True)
         self.step = 0
         self.collect: Optional[Dict[int, list]] = None      # set to {} to keep every request's output rows (tests)
 
@@ -259,17 +282,22 @@ class FoeStackRunner:
         S, mq = int(x.shape[0]), max(it.q_len for it in items)
         torch.cuda.synchronize()
         e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        cut = self._plan_cut(items)
         e0.record()
         h = x
         for l, layer in enumerate(self.layers):
+            if self.cache_format is not None:
+                h = self._block8(l, h, items, bt, ctx, ql, mq, cut)
+                continue
             kv = synth.PagedKV(self.k[l], self.v[l], bt, ctx, ql)
             # an iteration of decode tokens only takes the decode entry point (split-KV attention, weight streaming)
             h = layer.decode(h, kv) if mq == 1 else layer.prefill(h, kv, n_tokens=S, max_q_len=mq)
         e1.record()
         torch.cuda.synchronize()
-        status = self.layers[0].poll_status()
+        status = self.layers[0].poll_status() or (self.ops.poll_status() if self.cache_format is not None else 0)
         if status != 0:
             raise RuntimeError(f"device status {status}")
+        self._finish_cut(items, cut)
         if self.collect is not None:
             at = 0
             for it in items:
@@ -278,7 +306,47 @@ class FoeStackRunner:
         self.step += 1
         return e0.elapsed_time(e1) * 1e-3
 
+    # ---- the 8-bit cache
+    def _plan_cut(self, items: Sequence[BatchItem]) -> List[Tuple[int, List[int]]]:
+        """(index, pages taken for the move) of the batch's requests that are cut after this iteration."""
+        if self.kv_budget is None or self.pool is None:
+            return []
+        plan, width = [], pages_for(self.kv_budget)
+        for i, it in enumerate(items):
+            done = it.req.prefilling and it.context + it.q_len >= it.req.prompt_len
+            if done and it.req.prompt_len > self.kv_budget and width <= self.pool.free:
+                plan.append((i, self.pool.take(width)))
+        return plan
+
+    def _block8(self, l: int, h, items: Sequence[BatchItem], bt, ctx, ql, mq: int, cut):
+        torch = self.torch
+        n, nkv = len(items), self.shape.n_kv_heads
+        held = ctx - torch.tensor([it.req.dropped for it in items], dtype=torch.int32).to(self.device)
+        view = self.caches[l].view(bt, held, ql if mq > 1 else None, ctx)
+        if not cut:
+            return self.ops.block(self.layers[l], h, view, max_q_len=mq)
+        w = torch.zeros((n, nkv, self.max_pages_per_seq * PAGE), dtype=torch.float32, device=self.device)
+        h = self.ops.block(self.layers[l], h, view, max_q_len=mq, weights_in=w, weights_out=w, window=self.window)
+        rows = torch.tensor([i for i, _ in cut], device=self.device)
+        to = torch.tensor([pages for _, pages in cut], dtype=torch.int32, device=self.device)
+        lens = torch.empty(len(cut), dtype=torch.int32, device=self.device)
+        kept = torch.empty((len(cut), nkv, self.kv_budget), dtype=torch.int32, device=self.device)
+        self.ops.evict(self.caches[l].view(bt[rows], (held + ql)[rows]), w[rows], to, self.kv_budget, self.sink, self.recent, lens, kept)
+        return h
+
+    def _finish_cut(self, items: Sequence[BatchItem], cut) -> None:
+        for i, pages in cut:
+            r = items[i].req
+            need = pages_for(self.kv_budget + r.output_len)          # what it holds and what it may still write
+            grow = max(0, need - len(pages))
+            self.pool.give(r.pages[grow:])
+            r.pages = pages + r.pages[:grow]
+            r.dropped = r.prompt_len - self.kv_budget
+            self.cuts += 1
+
     def close(self):
+        if self.cache_format is not None:
+            self.ops.close()
         for layer in self.layers:
             layer.close()
 
