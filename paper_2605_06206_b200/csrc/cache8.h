@@ -43,7 +43,7 @@ struct Cache8AttendArgs {
   // partial results of a (sequence, KV head) whose keys are worked on by several CTAs
   float *part_o, *part_ml;
   int* split_done;
-  int* division;                    // chunks: first CTA of every block of a launch that splits keys
+  int4* division;                   // chunks whose keys are split: every block's first CTA, CTAs, first token and rows
   // for the accumulated weights (nullptr without them)
   float* lse;                       // [n_tokens][n_q] log2 of the row's softmax denominator
   float* logits;                    // single tokens: [n_seqs][n_q][logits_stride] scores in the log2 domain
@@ -93,10 +93,10 @@ struct Cache8Workspace {
 int launch_cache8_chunk(int fmt, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a,
                         const Cache8Workspace& ws, int min_q, int n_sms, cudaStream_t st);
 int cache8_expand_min_tokens(int group, int dh);    // group: query heads per KV head
-int cache8_chunk_division_ints();
+int cache8_chunk_max_split_blocks();
 size_t cache8_chunk_part_rows(int n_sms);
 cudaError_t cache8_chunk_configure();
-void launch_cache8_weights(int fmt, const Cache8WeightsArgs& w, cudaStream_t st);
+void launch_cache8_weights(int fmt, const Cache8WeightsArgs& w, int n_sms, cudaStream_t st);
 void launch_cache8_evict(int fmt, const Cache8EvictArgs& a, cudaStream_t st);
 cudaError_t cache8_evict_configure();
 

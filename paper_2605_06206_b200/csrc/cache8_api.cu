@@ -33,7 +33,7 @@ void lay_out(foe_cache* h, Arena* m) {
   m->take(&h->status, 1);                                  // zeroed at creation, with split_done behind it
   m->take(&h->split_done, h->split_done_count);
   m->take(&h->part_ml, rows * 2);
-  m->take(&h->division, cache8_chunk_division_ints());
+  m->take(&h->division, cache8_chunk_max_split_blocks());
   m->take(&h->part_o, rows * dhp);
   if (c.track_weights) {
     m->take(&h->lse, size_t(h->rows_max) * c.n_q_heads);
@@ -190,7 +190,7 @@ int cache8_attend(foe_cache* h, const foe_cache_view* v, const void* q, long lon
   if (w_out) {
     Cache8WeightsArgs w;
     w.a = a; w.weights_in = w_in; w.weights_out = w_out; w.weights_stride = w_stride; w.window = window;
-    launch_cache8_weights(h->cfg.format, w, st);
+    launch_cache8_weights(h->cfg.format, w, h->n_sms, st);
     n += 1;
   }
   return n;

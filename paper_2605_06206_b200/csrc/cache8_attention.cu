@@ -557,7 +557,7 @@ static void launch_decode_t(const CUtensorMap& tmK, const CUtensorMap& tmV, cons
   constexpr size_t smem = D8Smem<DH, NT>::kBytes;
   constexpr int kCtas = D8Cfg<NT>::kCtas;
   static_assert(kCtas * (smem + 1024) <= 228 * 1024, "CTAs per SM");
-  const long long most = ((long long)a.c.n_seqs * a.c.n_kv * a.c.max_kv_pages + kD8MinTiles - 1) / kD8MinTiles;
+  const long long most = (long long)a.c.n_seqs * a.c.n_kv * ((a.c.max_kv_pages + kD8MinTiles - 1) / kD8MinTiles);
   const int grid = int(most < (long long)kCtas * n_sms ? (most < 1 ? 1 : most) : (long long)kCtas * n_sms);
   launch_pdl(a.logits ? cache8_decode_kernel<FMT, DH, NT, true> : cache8_decode_kernel<FMT, DH, NT, false>, dim3(grid), dim3(D8Cfg<NT>::kThreads), smem, st, tmK, tmV, a);
 }

@@ -78,8 +78,8 @@ struct C8Launch {
 
 // A launch of fewer blocks than SMs gives every block as many CTAs as keep the longest of them short: `per` is the
 // smallest number of steps (at least kC8MinSteps) for which sum_i ceil(steps_i / per) CTAs fit the grid, and block i's
-// CTAs are first[i] .. first[i + 1] - 1.  Worked out by one warp of every CTA from the lengths on the device; the first CTA
-// leaves it for the joining kernel.
+// CTAs are first[i] .. first[i + 1] - 1.  Worked out by one warp of every CTA from the lengths on the device; a
+// block's first CTA leaves its part for the joining kernel (every block with a token has one).
 constexpr int kC8MaxSplitBlocks = 256, kC8MinSteps = 4;
 struct C8Division { int per, first[kC8MaxSplitBlocks + 1]; };
 __device__ __forceinline__ void c8_block_of(const Cache8Args& c, const C8Launch& lc, int pairs, int lin, int& b, int& pair, int& q0) {
@@ -168,8 +168,6 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     C8Division* d = reinterpret_cast<C8Division*>(smem);   // (before the tiles)
     if (warp == 0) c8_divide(c, lc, pairs, n_blocks, gridDim.x, d);
     __syncthreads();
-    if (blockIdx.x == 0)
-      for (int i = threadIdx.x; i <= n_blocks; i += CF::kThreads) a.division[i] = d->first[i];
     if (int(blockIdx.x) >= d->first[n_blocks]) return;
     int lo = 0, hi = n_blocks - 1;                         // the last block whose first CTA is not behind this one
     while (lo < hi) {
@@ -199,6 +197,7 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   const int rows_here = min(kC8Rows, q_len - q0);
   const int kv_len = ctx + q0 + rows_here;
   const int all_steps = (kv_len + kC8Keys - 1) / kC8Keys;
+  if (lc.split && split == 0 && threadIdx.x == 0) a.division[lin] = make_int4(int(blockIdx.x), n_splits, tok0, rows_here);
   const int step0 = split ? split * per_split : 0;
   const int n_steps = min(all_steps - step0, per_split);
 
@@ -643,21 +642,20 @@ __global__ void __launch_bounds__(kC8JoinThreads)
 cache8_join_kernel(const Cache8AttendArgs a, const C8Launch lc) {
   pdl_wait();
   pdl_launch_dependents();
-  __shared__ int red[kC8JoinThreads / 32];
   const Cache8Args& c = a.c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int n_tiles_q = c8_heads_per_block(c);
   const int pairs = c.n_q / n_tiles_q;
   const int lin = blockIdx.x, t = blockIdx.y;
-  const int first = a.division[lin], used = a.division[lin + 1] - first;
-  if (used < 2) return;                                    // (one CTA: it has written the output itself)
   int b, pair, q0;
   c8_block_of(c, lc, pairs, lin, b, pair, q0);
   const int head = pair * n_tiles_q + t;
-  const int q_len = c.q_lens[b];
-  const int start = c8_block_prefix(c.q_lens, b, red);
-  if ((long long)start + q_len > c.n_tokens) return;
-  const int rows_here = min(kC8Rows, q_len - q0);
+  const int q_len = c.q_lens[b], ctx = c.context_lens[b];
+  const int4 d = a.division[lin];
+  // (a block without tokens has left nothing)
+  if (q_len < lc.min_q || q_len >= lc.end_q || q_len > c.max_q_len || ctx < 0 || (long long)ctx + q_len > c.max_len || q0 >= q_len) return;
+  const int first = d.x, used = d.y, tok0 = d.z, rows_here = d.w;
+  if (used < 2 || (long long)tok0 - q0 + q_len > c.n_tokens) return;     // (one CTA: it has written the output itself)
   for (int row = blockIdx.z * (kC8JoinThreads / 32) + warp; row < rows_here; row += gridDim.z * (kC8JoinThreads / 32)) {
     auto prow = [&](int s) { return (size_t(first + s) * 2 + t) * kC8Rows + row; };
     float m = -INFINITY;
@@ -687,11 +685,11 @@ cache8_join_kernel(const Cache8AttendArgs a, const C8Launch lc) {
       }
     }
     const float inv = 1.f / l;
-    __nv_bfloat16* dst = a.out + (long long)(start + q0 + row) * a.out_stride + head * c.dh;
+    __nv_bfloat16* dst = a.out + (long long)(tok0 + row) * a.out_stride + head * c.dh;
 #pragma unroll
     for (int q = 0; q < DH / 32; ++q)
       if (q * 32 + lane < c.dh) dst[q * 32 + lane] = __float2bfloat16_rn(acc[q] * inv);
-    if (lane == 0 && a.lse) a.lse[size_t(start + q0 + row) * c.n_q + head] = m - kC8Shift + log2f(l);
+    if (lane == 0 && a.lse) a.lse[size_t(tok0 + row) * c.n_q + head] = m - kC8Shift + log2f(l);
   }
 }
 
@@ -764,7 +762,7 @@ cudaError_t cache8_chunk_configure() {
   return e;
 }
 
-int cache8_chunk_division_ints() { return kC8MaxSplitBlocks + 1; }
+int cache8_chunk_max_split_blocks() { return kC8MaxSplitBlocks; }
 size_t cache8_chunk_part_rows(int n_sms) { return size_t(n_sms) * 2 * kC8Rows; }
 
 // A call whose longest chunk has at least this many query rows per KV head (tokens x query heads of the head) expands its
@@ -778,7 +776,9 @@ template <int FMT, int DH>
 static int launch_chunk_t(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a, const Cache8Workspace& ws, int min_q, int n_sms, cudaStream_t st) {
   const Cache8Args& c = a.c;
   const int G = c.n_q / c.n_kv, tiles = G % 2 == 0 ? 2 : 1;
-  const bool expand = c.max_q_len >= cache8_expand_min_tokens(G, c.dh);
+  // (... and where there is little to do at all, the launch that expands costs more than it saves)
+  const long long page_reads = (long long)((c.max_q_len + kC8Rows - 1) / kC8Rows) * (c.n_q / tiles) * c.n_seqs * c.max_kv_pages;
+  const bool expand = c.max_q_len >= cache8_expand_min_tokens(G, c.dh) && page_reads >= 16LL * n_sms;
   const int long_q = (cache8_expand_min_tokens(G, c.dh) + 7) / 8;        // chunks from here on run on expanded tiles, if any (at least 6)
   // query blocks of a launch over n sequences of up to `longest` tokens; one CTA per SM, so a launch of fewer blocks
   // than that splits their keys.  Returns the CTAs.

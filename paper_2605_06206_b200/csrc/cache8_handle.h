@@ -10,7 +10,8 @@ struct foe_cache {
   void* memory;                         // the workspace that the pointers below are parts of
   int* status;
   float *part_o, *part_ml, *lse, *logits;
-  int *split_done, *division;
+  int* split_done;
+  int4* division;
   size_t split_done_count;
   long long logits_stride;
   foe::Cache8Workspace ws;

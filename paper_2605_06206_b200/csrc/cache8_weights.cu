@@ -46,24 +46,28 @@ cache8_weights_token_kernel(const Cache8WeightsArgs w) {
 }
 
 // ------------------------------------------------------------------------------------------- chunks
-constexpr int kWcThreads = 128;                  // four warps, 16 keys of every page each
-constexpr int kWcPages = 4;                      // pages of a block: what its query rows cost to bring in is spent once for them
-constexpr int kWcRows = 64;                      // query rows in shared memory at a time
-template <int FMT, int DH>
-__global__ void __launch_bounds__(kWcThreads)
+// PAGES of a block: what its query rows cost to bring in is spent once for four pages; one page where four would leave SMs
+// without a block, and then eight warps, four quarters of the page's keys times two halves of the query rows, whose sums
+// are added at the end.
+template <int FMT, int DH, int PAGES>
+__global__ void __launch_bounds__(PAGES == 1 ? 256 : 128)
 cache8_weights_chunk_kernel(const Cache8WeightsArgs w) {
   pdl_wait();
   pdl_launch_dependents();
+  constexpr int kHalves = PAGES == 1 ? 2 : 1, kWcThreads = 128 * kHalves;
+  constexpr int kWcRows = 64 * kHalves;          // query rows in shared memory at a time
   constexpr int NC = DH / 16;
   // Rows as B fragments: [row tile of 8][k-step][lane] two registers; factor, log2 of the denominator and position of every row
   __shared__ uint2 frag[kWcRows / 8][NC][32];
   __shared__ float row_f[kWcRows], row_lse[kWcRows];
   __shared__ int row_pos[kWcRows];
   __shared__ int red[kWcThreads / 32];
+  __shared__ float half_s[PAGES][64];            // sums of the second half of the warps
   const Cache8AttendArgs& a = w.a;
   const Cache8Args& c = a.c;
-  const int page0 = blockIdx.x * kWcPages, kvh = blockIdx.y, b = blockIdx.z;
+  const int page0 = blockIdx.x * PAGES, kvh = blockIdx.y, b = blockIdx.z;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+  const int quarter = warp & 3, half = warp >> 2;                   // (half: 0 with one page's worth of warps)
   const int G = c.n_q / c.n_kv;
   const int ctx = c.context_lens[b], q_len = c.q_lens[b];
   if (q_len < 0 || q_len > c.max_q_len || ctx < 0 || (long long)ctx + q_len > c.max_len) return;   // (reported by the attention)
@@ -71,13 +75,51 @@ cache8_weights_chunk_kernel(const Cache8WeightsArgs w) {
   if (page0 * 64 >= len) return;
   const int start = c8_block_prefix(c.q_lens, b, red);
   if ((long long)start + q_len > c.n_tokens) return;
-  const int n_pages = min(kWcPages, (len + 63) / 64 - page0);
+  const int n_pages = min(PAGES, (len + 63) / 64 - page0);
   // counted queries that see any key of the pages
   const int i_first = max(w.window > 0 ? max(q_len - w.window, 0) : 0, page0 * 64 - ctx);
   const int n_rows = (q_len - i_first) * G;
-  float sum[kWcPages][2];                                           // keys g and g + 8 of the warp's 16 keys of every page
+  float sum[PAGES][2];                                              // keys g and g + 8 of the warp's 16 keys of every page
+  int place[PAGES];                                                 // (page, head) index, or -1
+  float sk[PAGES];
 #pragma unroll
-  for (int i = 0; i < kWcPages; ++i) sum[i][0] = sum[i][1] = 0.f;
+  for (int i = 0; i < PAGES; ++i) {
+    sum[i][0] = sum[i][1] = 0.f;
+    const int page = i < n_pages ? c.block_table[size_t(b) * c.max_pages_per_seq + page0 + i] : -1;
+    place[i] = page < 0 || page >= c.num_pages ? -1 : page * c.n_kv + kvh;
+  }
+#pragma unroll
+  for (int i = 0; i < PAGES; ++i) sk[i] = place[i] >= 0 ? c.k_scales[place[i]] : 0.f;
+  // the warp's 16 keys of a page: rows g and g + 8 of them, the codes of chunks t4 and t4 + 4 ...
+  uint4 raw[NC / 4][2];
+  auto load_keys = [&](int ph) {
+#pragma unroll
+    for (int hh = 0; hh < NC / 4; ++hh) {
+      const int d0 = (t4 + 4 * hh) * 16;
+      raw[hh][0] = raw[hh][1] = make_uint4(0, 0, 0, 0);
+      if (d0 < c.dh && ph >= 0) {
+        const uint8_t* p = c.k_pages + (size_t(ph) * 64 + quarter * 16 + g) * c.dh + d0;
+        raw[hh][0] = *reinterpret_cast<const uint4*>(p);
+        raw[hh][1] = *reinterpret_cast<const uint4*>(p + 8 * c.dh);
+      }
+    }
+  };
+  // ... and as A fragments
+  uint32_t ka[NC][4];
+  auto decode_keys = [&]() {
+#pragma unroll
+    for (int hh = 0; hh < NC / 4; ++hh) {
+      const uint4 x = raw[hh][0], y = raw[hh][1];
+      const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        c8_decode_natural<FMT>(xs[i], ka[hh * 4 + i][0], ka[hh * 4 + i][2]);
+        c8_decode_natural<FMT>(ys[i], ka[hh * 4 + i][1], ka[hh * 4 + i][3]);
+      }
+    }
+  };
+  load_keys(place[0]);
+  if constexpr (PAGES == 1) decode_keys();
 
   for (int base = 0; base < n_rows; base += kWcRows) {
     const int here = min(kWcRows, n_rows - base);
@@ -99,6 +141,7 @@ cache8_weights_chunk_kernel(const Cache8WeightsArgs w) {
         }
         mx = max(mx, max(c8_absmax(v[hh][0]), c8_absmax(v[hh][1])));
       }
+      const float lse = there && t4 == 0 ? a.lse[size_t(start + i) * c.n_q + kvh * G + h] : 0.f;
       mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
       mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
       const int eq = c8_query_exp(mx);
@@ -113,39 +156,20 @@ cache8_weights_chunk_kernel(const Cache8WeightsArgs w) {
       }
       if (t4 == 0) {
         row_f[tile * 8 + g] = c8_pow2(eq) * a.scale_log2;
-        row_lse[tile * 8 + g] = there ? a.lse[size_t(start + i) * c.n_q + kvh * G + h] : 0.f;
+        row_lse[tile * 8 + g] = lse;
         row_pos[tile * 8 + g] = there ? ctx + i : -1;               // (a row that is none sees no key)
       }
     }
     __syncthreads();
 #pragma unroll
-    for (int pi = 0; pi < kWcPages; ++pi) {
-      if (pi >= n_pages) break;
-      const int page = c.block_table[size_t(b) * c.max_pages_per_seq + page0 + pi];
-      if (page < 0 || page >= c.num_pages) continue;
-      const size_t ph = size_t(page) * c.n_kv + kvh;
-      const int key0 = (page0 + pi) * 64 + warp * 16;
-      // this warp's 16 keys as A fragments: row g is key key0 + g, row g + 8 key key0 + g + 8; a lane holds the codes of
-      // chunks t4 and t4 + 4
-      uint32_t ka[NC][4];
-#pragma unroll
-      for (int hh = 0; hh < NC / 4; ++hh) {
-        const int d0 = (t4 + 4 * hh) * 16;
-        uint4 x = make_uint4(0, 0, 0, 0), y = x;
-        if (d0 < c.dh) {
-          const uint8_t* p = c.k_pages + (ph * 64 + warp * 16 + g) * c.dh + d0;
-          x = *reinterpret_cast<const uint4*>(p);
-          y = *reinterpret_cast<const uint4*>(p + 8 * c.dh);
-        }
-        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          c8_decode_natural<FMT>(xs[i], ka[hh * 4 + i][0], ka[hh * 4 + i][2]);
-          c8_decode_natural<FMT>(ys[i], ka[hh * 4 + i][1], ka[hh * 4 + i][3]);
-        }
+    for (int pi = 0; pi < PAGES; ++pi) {
+      if constexpr (PAGES > 1) {                                    // the next page's codes (or, for the next rows, the first's) are on their way
+        decode_keys();
+        load_keys(place[(pi + 1) % PAGES]);
       }
-      const float sk = c.k_scales[ph];
-      for (int tile = 0; tile * 8 < here; ++tile) {
+      if (place[pi] < 0) continue;
+      const int key0 = (page0 + pi) * 64 + quarter * 16;
+      for (int tile = half; tile * 8 < here; tile += kHalves) {
         float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < NC; ++k) {
@@ -155,7 +179,7 @@ cache8_weights_chunk_kernel(const Cache8WeightsArgs w) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {                               // columns 2 t4, 2 t4 + 1
           const int r = tile * 8 + t4 * 2 + e;
-          const float f = row_f[r] * sk, l = row_lse[r];
+          const float f = row_f[r] * sk[pi], l = row_lse[r];
           const int pos = row_pos[r];
           if (key0 + g <= pos) sum[pi][0] += fast_exp2(fmaf(s[e], f, -l));
           if (key0 + g + 8 <= pos) sum[pi][1] += fast_exp2(fmaf(s[e + 2], f, -l));
@@ -163,21 +187,36 @@ cache8_weights_chunk_kernel(const Cache8WeightsArgs w) {
       }
     }
   }
-  const size_t row = (size_t(b) * c.n_kv + kvh) * w.weights_stride;
 #pragma unroll
-  for (int pi = 0; pi < kWcPages; ++pi) {
+  for (int pi = 0; pi < PAGES; ++pi)
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      float v = sum[pi][e];
-      v += __shfl_xor_sync(0xffffffffu, v, 1);
-      v += __shfl_xor_sync(0xffffffffu, v, 2);
-      const int key = (page0 + pi) * 64 + warp * 16 + g + 8 * e;
-      if (t4 == 0 && pi < n_pages && key < len) w.weights_out[row + key] = w.weights_in[row + key] + v;
+      sum[pi][e] += __shfl_xor_sync(0xffffffffu, sum[pi][e], 1);
+      sum[pi][e] += __shfl_xor_sync(0xffffffffu, sum[pi][e], 2);
+      if (half == 1 && t4 == 0) half_s[pi][quarter * 16 + g + 8 * e] = sum[pi][e];
     }
+  __syncthreads();
+  const size_t row = (size_t(b) * c.n_kv + kvh) * w.weights_stride;
+  if (half == 0 && t4 == 0) {
+#pragma unroll
+    for (int pi = 0; pi < PAGES; ++pi)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int in_page = quarter * 16 + g + 8 * e, key = (page0 + pi) * 64 + in_page;
+        if (pi < n_pages && key < len) w.weights_out[row + key] = w.weights_in[row + key] + (sum[pi][e] + (kHalves == 2 ? half_s[pi][in_page] : 0.f));
+      }
   }
 }
 
-void launch_cache8_weights(int fmt, const Cache8WeightsArgs& w, cudaStream_t st) {
+template <int FMT, int DH>
+static void launch_weights_chunk_t(const Cache8WeightsArgs& w, int n_sms, cudaStream_t st) {
+  const Cache8Args& c = w.a.c;
+  const long long fours = (long long)((c.max_kv_pages + 3) / 4) * c.n_kv * c.n_seqs;
+  if (fours >= 2LL * n_sms) launch_pdl(cache8_weights_chunk_kernel<FMT, DH, 4>, dim3((c.max_kv_pages + 3) / 4, c.n_kv, c.n_seqs), dim3(128), 0, st, w);
+  else launch_pdl(cache8_weights_chunk_kernel<FMT, DH, 1>, dim3(c.max_kv_pages, c.n_kv, c.n_seqs), dim3(256), 0, st, w);
+}
+
+void launch_cache8_weights(int fmt, const Cache8WeightsArgs& w, int n_sms, cudaStream_t st) {
   const Cache8Args& c = w.a.c;
   if (c.n_seqs <= 0) return;
   if (!c.q_lens) {
@@ -185,14 +224,8 @@ void launch_cache8_weights(int fmt, const Cache8WeightsArgs& w, cudaStream_t st)
     launch_pdl(cache8_weights_token_kernel, grid, dim3(kWtThreads), 0, st, w);
     return;
   }
-  const dim3 grid((c.max_kv_pages + kWcPages - 1) / kWcPages, c.n_kv, c.n_seqs);
-  if (fmt == kC8E4M3) {
-    if (c.dh > 64) launch_pdl(cache8_weights_chunk_kernel<kC8E4M3, 128>, grid, dim3(kWcThreads), 0, st, w);
-    else launch_pdl(cache8_weights_chunk_kernel<kC8E4M3, 64>, grid, dim3(kWcThreads), 0, st, w);
-  } else {
-    if (c.dh > 64) launch_pdl(cache8_weights_chunk_kernel<kC8Int8, 128>, grid, dim3(kWcThreads), 0, st, w);
-    else launch_pdl(cache8_weights_chunk_kernel<kC8Int8, 64>, grid, dim3(kWcThreads), 0, st, w);
-  }
+  if (fmt == kC8E4M3) c.dh > 64 ? launch_weights_chunk_t<kC8E4M3, 128>(w, n_sms, st) : launch_weights_chunk_t<kC8E4M3, 64>(w, n_sms, st);
+  else c.dh > 64 ? launch_weights_chunk_t<kC8Int8, 128>(w, n_sms, st) : launch_weights_chunk_t<kC8Int8, 64>(w, n_sms, st);
 }
 
 }  // namespace foe
