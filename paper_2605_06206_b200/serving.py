@@ -280,14 +280,15 @@ class FoeStackRunner:
         bt, ctx, ql = bt.to(self.device), ctx.to(self.device), ql.to(self.device)
         x = self.inputs(items)
         S, mq = int(x.shape[0]), max(it.q_len for it in items)
-        torch.cuda.synchronize()
         e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
         cut = self._plan_cut(items)
+        plan8 = self._plan8(items, bt, ctx, ql, mq, cut) if self.cache_format is not None else None
+        torch.cuda.synchronize()
         e0.record()
         h = x
         for l, layer in enumerate(self.layers):
-            if self.cache_format is not None:
-                h = self._block8(l, h, items, bt, ctx, ql, mq, cut)
+            if plan8 is not None:
+                h = self._block8(l, h, plan8, mq)
                 continue
             kv = synth.PagedKV(self.k[l], self.v[l], bt, ctx, ql)
             # an iteration of decode tokens only takes the decode entry point (split-KV attention, weight streaming)
@@ -318,20 +319,31 @@ class FoeStackRunner:
                 plan.append((i, self.pool.take(width)))
         return plan
 
-    def _block8(self, l: int, h, items: Sequence[BatchItem], bt, ctx, ql, mq: int, cut):
+    def _plan8(self, items: Sequence[BatchItem], bt, ctx, ql, mq: int, cut) -> dict:
+        """What the layers' calls share, made before the iteration's clock starts: every layer's view, and of a cut the
+        sequences' views, destination pages and results."""
         torch = self.torch
         n, nkv = len(items), self.shape.n_kv_heads
         held = ctx - torch.tensor([it.req.dropped for it in items], dtype=torch.int32).to(self.device)
-        view = self.caches[l].view(bt, held, ql if mq > 1 else None, ctx)
-        if not cut:
-            return self.ops.block(self.layers[l], h, view, max_q_len=mq)
-        w = torch.zeros((n, nkv, self.max_pages_per_seq * PAGE), dtype=torch.float32, device=self.device)
-        h = self.ops.block(self.layers[l], h, view, max_q_len=mq, weights_in=w, weights_out=w, window=self.window)
-        rows = torch.tensor([i for i, _ in cut], device=self.device)
-        to = torch.tensor([pages for _, pages in cut], dtype=torch.int32, device=self.device)
-        lens = torch.empty(len(cut), dtype=torch.int32, device=self.device)
-        kept = torch.empty((len(cut), nkv, self.kv_budget), dtype=torch.int32, device=self.device)
-        self.ops.evict(self.caches[l].view(bt[rows], (held + ql)[rows]), w[rows], to, self.kv_budget, self.sink, self.recent, lens, kept)
+        plan = dict(views=[c.view(bt, held, ql if mq > 1 else None, ctx) for c in self.caches], cut=None)
+        if cut:
+            rows = torch.tensor([i for i, _ in cut], device=self.device)
+            table, lens = bt[rows].contiguous(), (held + ql)[rows].contiguous()
+            plan.update(cut=rows, sources=[c.view(table, lens) for c in self.caches],
+                        to=torch.tensor([pages for _, pages in cut], dtype=torch.int32, device=self.device),
+                        zeros=torch.zeros((n, nkv, self.max_pages_per_seq * PAGE), dtype=torch.float32, device=self.device),
+                        weights=torch.zeros((n, nkv, self.max_pages_per_seq * PAGE), dtype=torch.float32, device=self.device),
+                        new_lens=torch.empty(len(cut), dtype=torch.int32, device=self.device),
+                        kept=torch.empty((len(cut), nkv, self.kv_budget), dtype=torch.int32, device=self.device))
+        return plan
+
+    def _block8(self, l: int, h, p: dict, mq: int):
+        if p["cut"] is None:
+            return self.ops.block(self.layers[l], h, p["views"][l], max_q_len=mq)
+        h = self.ops.block(self.layers[l], h, p["views"][l], max_q_len=mq, weights_in=p["zeros"], weights_out=p["weights"],
+                           window=self.window)
+        self.ops.evict(p["sources"][l], p["weights"][p["cut"]], p["to"], self.kv_budget, self.sink, self.recent, p["new_lens"],
+                       p["kept"])
         return h
 
     def _finish_cut(self, items: Sequence[BatchItem], cut) -> None:

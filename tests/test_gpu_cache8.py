@@ -715,3 +715,76 @@ def test_offsets_beyond_32_bits():
     got = ref.Pool(pool.k_pages[tail], pool.k_scales[tail], "e4m3")
     assert torch.equal(got.num, kp.num) and torch.equal(got.scale, kp.scale)
     assert ops.poll_status() == 0
+
+
+@pytest.mark.parametrize("ctx,q", [([100, 70], None), ([100, 70], [9, 130]), ([10, 70], [900, 2])])
+def test_non_finite_queries_stay_in_their_row_and_head(ctx, q):
+    lens = q or [1, 1]
+    s = Setup(4, 2, 128, "e4m3", [a + b for a, b in zip(ctx, lens)], seed=70)
+    s.fill([a + b for a, b in zip(ctx, lens)])
+    x = s.randn(sum(lens), 4, 128)
+    clean = s.ops.attend(x.cuda(), s.view(ctx, q)).cpu()
+    bad = x.clone()
+    bad[0, 1, 5] = math.nan
+    bad[lens[0], 2, 127] = math.inf
+    got = s.ops.attend(bad.cuda(), s.view(ctx, q)).cpu()
+    hit = torch.zeros(sum(lens), 4, dtype=torch.bool)
+    hit[0, 1] = hit[lens[0], 2] = True
+    assert bool(got[hit].isnan().all())
+    assert torch.equal(got[~hit], clean[~hit])
+
+
+def test_two_handles_on_two_streams_at_once():
+    """Handles do not share anything: the same calls, interleaved on two streams, give what they give alone."""
+    a = Setup(8, 2, 128, "e4m3", [3000, 900], seed=71)
+    b = Setup(8, 2, 128, "int8", [2500, 77], seed=72)
+    a.fill([3000, 900]), b.fill([2500, 77])
+    xa, xb = a.randn(2, 8, 128).cuda(), b.randn(700, 8, 128).cuda()
+    va, vb = a.view([2999, 899]), b.view([1850, 27], [650, 50])
+    wa, wb = torch.zeros(2, 2, a.width * PAGE, device="cuda"), torch.zeros(2, 2, b.width * PAGE, device="cuda")
+    want_a = a.ops.attend(xa, va, weights_in=wa, weights_out=wa).clone()
+    want_b = b.ops.attend(xb, vb, max_q_len=650, weights_in=wb, weights_out=wb, window=8).clone()
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    outs = []
+    for _ in range(10):
+        oa, ob, na, nb = torch.empty_like(want_a), torch.empty_like(want_b), torch.zeros_like(wa), torch.zeros_like(wb)
+        torch.cuda.current_stream().synchronize()
+        a.ops.attend(xa, va, out=oa, weights_in=na, weights_out=na, stream=s1)
+        b.ops.attend(xb, vb, out=ob, max_q_len=650, weights_in=nb, weights_out=nb, window=8, stream=s2)
+        outs.append((oa, ob, na, nb))
+    torch.cuda.synchronize()
+    for oa, ob, na, nb in outs:
+        assert torch.equal(oa, want_a) and torch.equal(ob, want_b) and torch.equal(na, wa) and torch.equal(nb, wb)
+
+
+def test_eviction_in_a_graph_and_on_another_stream():
+    lens, budget = [500, 90], 128
+    s = Setup(2, 2, 64, "int8", lens, seed=73, extra_pages=4)
+    s.fill(lens)
+    w = torch.rand(2, 2, s.width * PAGE, generator=s.g)
+    to, ctx = s.spare[:4].view(2, 2), i32(lens)
+    view = s.pool.view(s.table.cuda(), ctx)
+    kept, new_lens, w_out = torch.zeros(2, 2, budget, dtype=torch.int32, device="cuda"), i32([0, 0]), torch.zeros(2, 2, 128, device="cuda")
+    wd, tod = w.cuda(), to.cuda()
+    kp, vp = s.refs()
+    want, want_lens = ref.evict(kp, vp, s.table, lens, w, to, budget, 4, 20)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    s.ops.evict(view, wd, tod, budget, 4, 20, new_lens, kept, w_out, stream=stream)
+    stream.synchronize()
+    s.same(kp, vp)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s.ops.evict(view, wd, tod, budget, 4, 20, new_lens, kept, w_out)
+    kept.zero_(), new_lens.zero_(), w_out.zero_()
+    ctx.copy_(i32([300, 40]))                                       # the captured call follows the lengths on the device
+    graph.replay()
+    torch.cuda.synchronize()
+    kp, vp = s.refs()
+    want, want_lens = ref.evict(kp, vp, s.table, [300, 40], w, to, budget, 4, 20)
+    assert new_lens.tolist() == want_lens == [128, 40]
+    for b in range(2):
+        for h in range(2):
+            assert kept[b, h, :want_lens[b]].tolist() == want[b][h]
+    s.same(kp, vp)
