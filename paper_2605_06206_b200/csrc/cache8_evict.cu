@@ -25,6 +25,11 @@ __device__ __forceinline__ uint32_t weight_key(float x) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
+// the weight a key stands for (a NaN or -0 comes back as some NaN or +0)
+__device__ __forceinline__ float key_weight(uint32_t u) {
+  return __uint_as_float(u == 0u ? 0x7fc00000u : ((u & 0x80000000u) ? (u & 0x7fffffffu) : ~u));
+}
+
 // sum of v over the threads before this one (every warp adds up the other warps' sums by itself)
 __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* warp_sums) {
   static_assert(kEvThreads == 1024, "one warp sum per lane");
@@ -129,7 +134,27 @@ cache8_select_kernel(const Cache8EvictArgs a) {
   // length odd so that the threads of a warp read different banks; one scan gives every run its place.
   const int run = ((len + kEvThreads - 1) / kEvThreads) | 1;
   const int j0 = min(tid * run, len), j1 = min(j0 + run, len);
-  uint32_t n_keep = 0, n_eq = 0;                           // kept whatever the ties do; equal to the last one kept
+  if constexpr (STAGED) {
+    static_assert(kEvKeysMax / kEvThreads < 64, "a run's positions are the bits of one word");
+    unsigned long long keep = 0, eq = 0;                   // kept whatever the ties do; equal to the last one kept
+    for (int j = j0; j < j1; ++j) {
+      const uint32_t u = keys[j];
+      const bool forced = j < lo || j >= hi;
+      keep |= (unsigned long long)(forced || (want > 0 && u > prefix)) << (j - j0);
+      eq |= (unsigned long long)(!forced && want > 0 && u == prefix) << (j - j0);
+    }
+    uint32_t at = block_scan(__popcll(keep), warp_sums);
+    const uint32_t eq_before = block_scan(__popcll(eq), warp_sums);
+    at += min(eq_before, uint32_t(k));
+    for (uint32_t n = eq_before; eq && n < uint32_t(k); ++n, eq &= eq - 1) keep |= eq & -eq;      // the lowest ties that still fit
+    for (; keep; keep &= keep - 1, ++at) {
+      const int j = j0 + __ffsll(keep) - 1;
+      kept[at] = j;
+      if (wout) wout[at] = key_weight(keys[j]);
+    }
+    return;
+  }
+  uint32_t n_keep = 0, n_eq = 0;
   for (int j = j0; j < j1; ++j) {
     if (j < lo || j >= hi) { ++n_keep; continue; }
     const uint32_t u = key(j);
