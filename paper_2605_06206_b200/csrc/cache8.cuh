@@ -134,6 +134,12 @@ __device__ __forceinline__ int c8_query_exp(uint32_t amax_bits) {
 // sum of q_lens[0 .. b) by the whole block (every thread gets it); `red` = one int per warp of shared memory
 __device__ __forceinline__ int c8_block_prefix(const int* q_lens, int b, int* red) {
   int s = 0;
+  if (b <= 64) {                                           // few: every warp by itself
+    const int i = threadIdx.x & 31;
+    if (i < b) s = max(q_lens[i], 0);
+    if (i + 32 < b) s += max(q_lens[i + 32], 0);
+    return __reduce_add_sync(0xffffffffu, s);
+  }
   for (int i = threadIdx.x; i < b; i += blockDim.x) s += max(q_lens[i], 0);
   s = __reduce_add_sync(0xffffffffu, s);
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;

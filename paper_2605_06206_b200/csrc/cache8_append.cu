@@ -26,6 +26,12 @@ cache8_append_token_kernel(const Cache8AppendArgs a) {
   const int kvh = int(item % c.n_kv);
   const int b = int((item / c.n_kv) % c.n_seqs);
   const bool is_v = item >= (long long)c.n_seqs * c.n_kv;
+  // (the row's values are on their way while its place is looked up)
+  const Cache8Rows& lay = is_v ? a.v_lay : a.k_lay;
+  const __nv_bfloat16* src = (is_v ? a.v : a.k) + (b >> 6) * lay.tile + (b & 63) * lay.row + kvh * lay.head;
+  const bool have = lane * 4 < c.dh;                       // four elements a lane (head_dim is 64, 96 or 128)
+  uint2 x = make_uint2(0, 0);
+  if (have) x = __ldg(reinterpret_cast<const uint2*>(src + lane * 4));
   const int pos = c.context_lens[b];
   if (pos < 0 || pos >= c.max_len) {
     if (lane == 0) atomicExch(c.status, kStatusBounds);
@@ -40,11 +46,6 @@ cache8_append_token_kernel(const Cache8AppendArgs a) {
   const int row = pos & 63;
   float* scale_p = (is_v ? c.v_scales : c.k_scales) + ph;
   uint32_t* codes = reinterpret_cast<uint32_t*>((is_v ? c.v_pages : c.k_pages) + ph * 64 * c.dh);
-  const Cache8Rows& lay = is_v ? a.v_lay : a.k_lay;
-  const __nv_bfloat16* src = (is_v ? a.v : a.k) + (b >> 6) * lay.tile + (b & 63) * lay.row + kvh * lay.head;
-  const bool have = lane * 4 < c.dh;                       // four elements a lane (head_dim is 64, 96 or 128)
-  uint2 x = make_uint2(0, 0);
-  if (have) x = *reinterpret_cast<const uint2*>(src + lane * 4);
   const float held = row > 0 ? *scale_p : 1.f;
   const uint32_t m2 = absmax_bf16x2(x.x, x.y);
   const uint32_t amax = __reduce_max_sync(0xffffffffu, max(m2 & 0xffffu, m2 >> 16));
@@ -93,36 +94,38 @@ cache8_append_chunk_kernel(const Cache8AppendArgs a, const int blocks_per_seq) {
   const int blk = bad ? 0 : (ctx >> 6) + slot;
   if (!bad && blk * 64 >= ctx + q_len) return;
   const int tok0 = c8_block_prefix(c.q_lens, b, red);
-  if (bad || tok0 + q_len > c.n_tokens) {                  // the call's lengths disagree with what the host was told
+  if (bad || (long long)tok0 + q_len > c.n_tokens) {       // the call's lengths disagree with what the host was told
     if (threadIdx.x == 0) atomicExch(c.status, kStatusBounds);
     return;
   }
-  const int page = c.block_table[size_t(b) * c.max_pages_per_seq + blk];
-  if (page < 0 || page >= c.num_pages) {
-    if (threadIdx.x == 0) atomicExch(c.status, kStatusBounds);
-    return;
-  }
+  // the rows' values are on their way while their place is looked up
   const int first = max(ctx - blk * 64, 0);                // rows the page holds already
   const int last = min(ctx + q_len - blk * 64, 64);        // rows [first, last) are new
-  const size_t ph = size_t(page) * c.n_kv + kvh;
-  float* scale_p = (is_v ? c.v_scales : c.k_scales) + ph;
-  uint2* codes = reinterpret_cast<uint2*>((is_v ? c.v_pages : c.k_pages) + ph * 64 * DH);
   const Cache8Rows& lay = is_v ? a.v_lay : a.k_lay;
   const __nv_bfloat16* src = (is_v ? a.v : a.k) + kvh * lay.head;
   const int tok_row0 = tok0 + blk * 64 - ctx;              // token of the page's row 0 (rows before `first` are older)
   uint4 x[PER];
-  uint32_t m2 = 0;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int p = i * kApThreads + threadIdx.x, row = p / CH, ch = p - row * CH;
     x[i] = make_uint4(0, 0, 0, 0);
     if (row >= first && row < last) {
       const int t = tok_row0 + row;
-      x[i] = *reinterpret_cast<const uint4*>(src + (t >> 6) * lay.tile + (t & 63) * lay.row + ch * 8);
+      x[i] = __ldg(reinterpret_cast<const uint4*>(src + (t >> 6) * lay.tile + (t & 63) * lay.row + ch * 8));
     }
-    m2 = __vmaxu2(m2, __vmaxu2(absmax_bf16x2(x[i].x, x[i].y), absmax_bf16x2(x[i].z, x[i].w)));
   }
+  const int page = c.block_table[size_t(b) * c.max_pages_per_seq + blk];
+  if (page < 0 || page >= c.num_pages) {
+    if (threadIdx.x == 0) atomicExch(c.status, kStatusBounds);
+    return;
+  }
+  const size_t ph = size_t(page) * c.n_kv + kvh;
+  float* scale_p = (is_v ? c.v_scales : c.k_scales) + ph;
   const float held = first > 0 ? *scale_p : 1.f;
+  uint2* codes = reinterpret_cast<uint2*>((is_v ? c.v_pages : c.k_pages) + ph * 64 * DH);
+  uint32_t m2 = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) m2 = __vmaxu2(m2, __vmaxu2(absmax_bf16x2(x[i].x, x[i].y), absmax_bf16x2(x[i].z, x[i].w)));
   const uint32_t wmax = __reduce_max_sync(0xffffffffu, max(m2 & 0xffffu, m2 >> 16));
   if ((threadIdx.x & 31) == 0) redm[threadIdx.x >> 5] = wmax;
   __syncthreads();                                         // (also: `held` has been read by every thread)
