@@ -884,13 +884,19 @@ foe_status foe_cache_block(foe_layer* L, foe_cache* h, const void* x, const foe_
   if (s == FOE_OK) s = cache8_check_weights(h, view, weights_in, weights_out, weights_stride, window);
   if (s != FOE_OK) return s;
   if (view->n_seqs > L->cfg.max_seqs || rows > (decode ? L->cfg.max_seqs : L->cfg.max_tokens)) return FOE_ERR_SHAPE;
-  if (rows == 0) { L->launches = 0; L->last_tokens = 0; return FOE_OK; }
-  if (!x || !out) return FOE_ERR_NULL;
+  if (rows > 0 && (!x || !out)) return FOE_ERR_NULL;
   if (misaligned(x, 16) || misaligned(out, 16)) return FOE_ERR_SHAPE;
-  if (x == out) return FOE_ERR_UNSUPPORTED;
+  if (rows > 0 && x == out) return FOE_ERR_UNSUPPORTED;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (rows == 0) {                                     // no token: only the weights' copy, where they are asked for
+    L->launches = 0;
+    L->last_tokens = 0;
+    return weights_out && view->n_seqs > 0 ? foe_cache_attend(h, nullptr, h->cfg.n_q_heads * h->cfg.head_dim, view, nullptr,
+                                                              h->cfg.n_q_heads * h->cfg.head_dim, weights_in, weights_out, weights_stride, window, stream)
+                                           : FOE_OK;
+  }
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev != h->device) return FOE_ERR_UNSUPPORTED;
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
   h->last_stream = st;
   // what the shared launch sequence reads of a bf16 cache; K and V of the new tokens go to the staging rows
   foe_kv_cache kv;

@@ -135,6 +135,20 @@ def test_block_refusals_and_bad_positions():
     assert s.layer.poll_status() == 0 and s.ops.poll_status() == 0
 
 
+def test_block_without_tokens():
+    s = Both(SHAPES["dh64"], "e4m3", 2, 300, seed=7)
+    s.step([0, 0], [70, 100], 40)
+    empty = torch.zeros(4, 0, 256, dtype=torch.bfloat16, device="cuda")
+    w, w_out = torch.rand(2, 4, 320, device="cuda"), torch.zeros(2, 4, 320, device="cuda")
+    before = [t.clone() for t in (s.pool.k_pages, s.pool.k_scales)]
+    out = s.ops.block(s.layer, empty, s.pool.view(s.table.cuda(), i32([70, 100]), i32([0, 0])), weights_in=w, weights_out=w_out)
+    assert out.shape[1] == 0 and s.layer.poll_status() == 0 and s.ops.poll_status() == 0
+    assert torch.equal(w_out[0, :, :70], w[0, :, :70]) and torch.equal(w_out[1, :, :100], w[1, :, :100])
+    assert bool((w_out[0, :, 70:] == 0).all()) and torch.equal(before[0], s.pool.k_pages) and torch.equal(before[1], s.pool.k_scales)
+    none = s.pool.view(s.table[:0].cuda(), i32([]))
+    assert s.ops.block(s.layer, empty, none).shape[1] == 0
+
+
 def test_block_decode_replayed_from_a_graph():
     s = Both(SHAPES["dh64"], "int8", 2, 300, seed=6)
     s.step([0, 0], [70, 100], 30)
