@@ -53,7 +53,8 @@ struct D8Smem {
   static constexpr int kRows = 8 * NT;
   static constexpr int kMoOff = kRing;
   static constexpr int kMmOff = kMoOff + kRows * kPitch * 4;                     // [warps][kRows] maxima, then sums
-  static constexpr int kScaleOff = kMmOff + 2 * D8Cfg<NT>::kWarps * kRows * 4;   // [64] K scale, log2 V scale, 1 / V scale of the last pages
+  static constexpr int kRowOff = kMmOff + 2 * D8Cfg<NT>::kWarps * kRows * 4;     // [kRows] maxima, then sums, of the segment
+  static constexpr int kScaleOff = kRowOff + 2 * kRows * 4;                      // [64] K scale, log2 V scale, 1 / V scale of the last pages
   static constexpr int kBarOff = kScaleOff + 64 * 16;
   static constexpr int kMiscOff = kBarOff + 2 * kD8Stages * 8;
   static constexpr size_t kBytes = size_t(kMiscOff) + 16 + 1024;
@@ -85,6 +86,8 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   float* mo = reinterpret_cast<float*>(smem + SM::kMoOff);
   float* mm = reinterpret_cast<float*>(smem + SM::kMmOff);
   float* ml = mm + CF::kWarps * SM::kRows;
+  float* row_m = reinterpret_cast<float*>(smem + SM::kRowOff);
+  float* row_l = row_m + SM::kRows;
   float4* scales = reinterpret_cast<float4*>(smem + SM::kScaleOff);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + SM::kBarOff);
   uint64_t* empty = full + kD8Stages;
@@ -257,6 +260,13 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       qs[n][1] = __shfl_sync(0xffffffffu, f, t4 * 8 + 4);
     }
 
+    // the next pair's queries, which this CTA probably needs when it is done here, come near
+    if (!c.q_lens && w.page + len >= w.np) {
+      const int kn = kvh + 1 == c.n_kv ? 0 : kvh + 1, bn = kvh + 1 == c.n_kv ? b + 1 : b;
+      if (bn < c.n_seqs && lane < G)
+        asm volatile("prefetch.global.L1 [%0];" ::"l"(a.q + (long long)bn * a.q_stride + (kn * G + lane) * a.q_head_stride + warp * (c.dh / 4)));
+    }
+
     float o[NT][NC][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -388,6 +398,18 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         }
       }
     d8_bar<CT>();
+    if (ctid < SM::kRows) {                                        // row r of the segment: maximum and sum (read after the rounds)
+      float m = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int q = 0; q < CF::kWarps; ++q) m = fmaxf(m, mm[q * SM::kRows + ctid]);
+#pragma unroll
+      for (int q = 0; q < CF::kWarps; ++q) {
+        const float mq = mm[q * SM::kRows + ctid];
+        l += (mq == -INFINITY ? 0.f : fast_exp2(mq - m)) * ml[q * SM::kRows + ctid];
+      }
+      row_m[ctid] = m;
+      row_l[ctid] = l;
+    }
     float f[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -422,40 +444,25 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       }
       d8_bar<CT>();
     }
-    // row r of the segment: maximum m, sum l, unnormalised output mo[r][.]
-    auto row_ml = [&](int r, float& m, float& l) {
-      m = -INFINITY;
-      l = 0.f;
-#pragma unroll
-      for (int q = 0; q < CF::kWarps; ++q) m = fmaxf(m, mm[q * SM::kRows + r]);
-#pragma unroll
-      for (int q = 0; q < CF::kWarps; ++q) {
-        const float mq = mm[q * SM::kRows + r];
-        l += (mq == -INFINITY ? 0.f : fast_exp2(mq - m)) * ml[q * SM::kRows + r];
-      }
-    };
+    // the segment's rows: maximum row_m, sum row_l, unnormalised output mo[row][.]; a thread takes one column of every
+    // (CT / DH)-th row
+    const int d = ctid % DH;
     if (n_segs == 1) {
       // the whole pair was this segment: normalise and store
-      for (int q = ctid; ok && q < G * DH; q += CT) {
-        const int r = q / DH, d = q - r * DH;
-        float m, l;
-        row_ml(r, m, l);
+      for (int r = ctid / DH; ok && r < G; r += CT / DH) {
         if (d < c.dh && tok_ok)                                    // (a 96-wide head is computed zero-padded to 128)
-          a.out[(long long)tok * a.out_stride + (kvh * G + r) * c.dh + d] = __float2bfloat16_rn(mo[r * SM::kPitch + d] / l);
-        if (d == 0 && a.lse && tok_ok) a.lse[size_t(tok) * c.n_q + kvh * G + r] = m - kD8Shift + log2f(l);
+          a.out[(long long)tok * a.out_stride + (kvh * G + r) * c.dh + d] = __float2bfloat16_rn(mo[r * SM::kPitch + d] * (1.f / row_l[r]));
+        if (d == 0 && a.lse && tok_ok) a.lse[size_t(tok) * c.n_q + kvh * G + r] = row_m[r] - kD8Shift + log2f(row_l[r]);
       }
     } else {
       // A segment whose wait ran out writes no partial state but still takes its ticket: the counter of its pair
       // returns to zero and the handle stays usable (this call's output is not; the status word says so).
       const size_t slot = size_t(blockIdx.x) * 2 + (seg == 0 ? 1 : 0);
-      for (int q = ctid; ok && q < G * DH; q += CT) {
-        const int r = q / DH, d = q - r * DH;
+      for (int r = ctid / DH; ok && r < G; r += CT / DH) {
         a.part_o[(slot * 16 + r) * DH + d] = mo[r * SM::kPitch + d];
         if (d == 0) {
-          float m, l;
-          row_ml(r, m, l);
-          a.part_ml[(slot * 16 + r) * 2] = m;
-          a.part_ml[(slot * 16 + r) * 2 + 1] = l;
+          a.part_ml[(slot * 16 + r) * 2] = row_m[r];
+          a.part_ml[(slot * 16 + r) * 2 + 1] = row_l[r];
         }
       }
       pend_b[n_pend & 1] = b; pend_kvh[n_pend & 1] = kvh; pend_c0[n_pend & 1] = c_first; pend_n[n_pend & 1] = n_segs; pend_tok[n_pend & 1] = tok;

@@ -33,53 +33,51 @@ __device__ __forceinline__ int dc_pages(const Args& a, int b, int* kv_len) {
 template <int GAP = 0, bool SINGLES = false, typename Args>
 __device__ __forceinline__ bool dc_begin(const Args& a, int min_tiles, DcWalk& w) {
   const int lane = threadIdx.x & 31;
-  int sum = 0, np_first = 0, kl_first = 0;        // (the first 32 sequences' values are kept for the search below)
-  for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
-    int kl = 0;
-    const int np = b0 + lane < a.n_seqs ? dc_pages<SINGLES>(a, b0 + lane, &kl) : 0;
-    if (b0 == 0) { np_first = np; kl_first = kl; }
-    sum += np + (np > 0 ? GAP : 0);
+  // a lane takes `share` consecutive sequences: one pass for their entries, one scan over the lanes, and the lane whose
+  // sequences hold the range's start looks for it among them
+  const int share = (a.n_seqs + 31) >> 5;
+  const int b_lo = min(lane * share, a.n_seqs), b_hi = min(b_lo + share, a.n_seqs);
+  int mine = 0, kl = 0, np = 0;                  // (with up to 32 sequences kl and np are the lane's one)
+#pragma unroll 4                                   // (the lengths' loads in flight together)
+  for (int b = b_lo; b < b_hi; ++b) {
+    np = dc_pages<SINGLES>(a, b, &kl);
+    mine += np + (np > 0 ? GAP : 0);
   }
+  int incl = mine;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  const int T = sum * a.n_kv;
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += v;
+  }
+  const int T = __shfl_sync(0xffffffffu, incl, 31) * a.n_kv;
   w.per = max(min_tiles, (T + int(gridDim.x) - 1) / int(gridDim.x));
   const long long t0 = (long long)blockIdx.x * w.per;
   if (t0 >= T) return false;
   w.t = int(t0);
   w.t_end = min(T, w.t + w.per);
-  int base = 0;                                  // entries (per KV head) of the sequences before this chunk of 32
-  for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
-    int kl = kl_first;
-    const int np = b0 == 0 ? np_first : (b0 + lane < a.n_seqs ? dc_pages<SINGLES>(a, b0 + lane, &kl) : 0);
-    const int size = np + (np > 0 ? GAP : 0);
-    int incl = size;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += v;
+  int first = a.n_kv * (incl - mine), b = b_lo;    // first entry of sequence b
+  const bool hit = mine > 0 && w.t >= first && w.t < first + a.n_kv * mine;
+  if (hit && share > 1) {
+    for (;; ++b) {
+      np = dc_pages<SINGLES>(a, b, &kl);
+      const int size = a.n_kv * (np + (np > 0 ? GAP : 0));
+      if (w.t < first + size) break;             // (before b_hi: the lane's entries hold w.t)
+      first += size;
     }
-    const int first = a.n_kv * (base + incl - size);
-    const bool hit = np > 0 && w.t >= first && w.t < first + a.n_kv * size;
-    const uint32_t m = __ballot_sync(0xffffffffu, hit);
-    if (m) {
-      const int src = __ffs(m) - 1;
-      w.b = b0 + src;
-      w.seq_first = __shfl_sync(0xffffffffu, first, src);
-      w.np = __shfl_sync(0xffffffffu, np, src);
-      w.kv_len = __shfl_sync(0xffffffffu, kl, src);
-      const int rem = w.t - w.seq_first;
-      w.kvh = rem / (w.np + GAP);
-      w.page = rem - w.kvh * (w.np + GAP) - GAP;
-      if (GAP > 0 && w.page < 0) {                 // the range starts in front of a pair
-        w.t -= w.page;
-        w.page = 0;
-      }
-      return GAP == 0 || w.t < w.t_end;
-    }
-    base += __shfl_sync(0xffffffffu, incl, 31);
   }
-  return false;                                  // (not reached: t0 < T)
+  const int src = __ffs(__ballot_sync(0xffffffffu, hit)) - 1;
+  w.b = __shfl_sync(0xffffffffu, b, src);
+  w.seq_first = __shfl_sync(0xffffffffu, first, src);
+  w.np = __shfl_sync(0xffffffffu, np, src);
+  w.kv_len = __shfl_sync(0xffffffffu, kl, src);
+  const int rem = w.t - w.seq_first;
+  w.kvh = rem / (w.np + GAP);
+  w.page = rem - w.kvh * (w.np + GAP) - GAP;
+  if (GAP > 0 && w.page < 0) {                   // the range starts in front of a pair
+    w.t -= w.page;
+    w.page = 0;
+  }
+  return GAP == 0 || w.t < w.t_end;
 }
 
 // pages of the segment that starts at the current entry
