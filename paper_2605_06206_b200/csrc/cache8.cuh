@@ -108,6 +108,15 @@ __device__ __forceinline__ uint32_t c8_rescale4(uint32_t w, float factor) {
 }
 
 // ---- shared by the attention kernels
+// A page of one head in shared memory, as its TMA box leaves it: 64 rows of 64 bytes (64-wide heads) or 128 bytes (a 96-wide
+// head is padded with zeros), the 16-byte chunk index XOR-ed with the row so that eight rows' equal chunks, and the chunks
+// of two rows, hit every bank once.
+template <int DH>
+constexpr int c8_tile_bytes() { return 64 * (DH > 64 ? 128 : 64); }
+template <int DH>
+__device__ __forceinline__ uint32_t c8_code_off(int row, int chunk) {
+  return DH > 64 ? uint32_t(row * 128 + (((chunk ^ row) & 7) << 4)) : uint32_t(row * 64 + (((chunk ^ (row >> 1)) & 3) << 4));
+}
 __device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"

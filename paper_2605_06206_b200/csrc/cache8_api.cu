@@ -54,16 +54,16 @@ void lay_out(foe_cache* h, Arena* m) {
   }
 }
 
-// codes of all pages as rows of head_dim bytes; a box is one page of one head, rows padded with zeros to 128 bytes
+// codes of all pages as rows of head_dim bytes; a box is one page of one head (c8_code_off gives its layout)
 bool make_code_map(CUtensorMap* m, const void* base, uint64_t rows, uint64_t dh) {
   EncodeTiledFn fn = get_encode_fn();
   if (!fn) return false;
   const cuuint64_t gdim[2] = {dh, rows};
   const cuuint64_t gstride[1] = {dh};
-  const cuuint32_t box[2] = {128, 64};
+  const cuuint32_t box[2] = {dh > 64 ? 128u : 64u, 64};
   const cuuint32_t estr[2] = {1, 1};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+            dh > 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // 16-bit operand tiles: rows of `width` values, a box is 64 rows of 64 of them

@@ -33,7 +33,7 @@
 
 namespace foe {
 
-constexpr int kD8Stages = 3;
+template <int DH> constexpr int d8_stages() { return DH > 64 ? 3 : 6; }      // about 48 KB in flight
 constexpr int kD8MinTiles = 2;                   // fewest pages per CTA
 constexpr int kD8Gap = 6;                        // what starting a pair costs, in pages (decode_walk.cuh)
 constexpr float kD8Shift = 6.f;                  // P' = 2^(t - m + shift)
@@ -47,8 +47,9 @@ template <int NT> struct D8Cfg {                 // NT: tiles of 8 heads
 
 template <int DH, int NT>
 struct D8Smem {
-  static constexpr int kTile = 64 * 128;         // codes of a page of one head, rows padded to 128 bytes by the TMA box
-  static constexpr int kRing = kD8Stages * 2 * kTile;
+  static constexpr int kStages = d8_stages<DH>();
+  static constexpr int kTile = c8_tile_bytes<DH>();                              // codes of a page of one head
+  static constexpr int kRing = kStages * 2 * kTile;
   static constexpr int kPitch = DH + 8;
   static constexpr int kRows = 8 * NT;
   static constexpr int kMoOff = kRing;
@@ -56,7 +57,7 @@ struct D8Smem {
   static constexpr int kRowOff = kMmOff + 2 * D8Cfg<NT>::kWarps * kRows * 4;     // [kRows] maxima, then sums, of the segment
   static constexpr int kScaleOff = kRowOff + 2 * kRows * 4;                      // [64] K scale, log2 V scale, 1 / V scale of the last pages
   static constexpr int kBarOff = kScaleOff + 64 * 16;
-  static constexpr int kMiscOff = kBarOff + 2 * kD8Stages * 8;
+  static constexpr int kMiscOff = kBarOff + 2 * kStages * 8;
   static constexpr size_t kBytes = size_t(kMiscOff) + 16 + 1024;
 };
 
@@ -79,6 +80,7 @@ __global__ void __launch_bounds__(D8Cfg<NT>::kThreads, D8Cfg<NT>::kCtas)
 cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const Cache8AttendArgs a) {
   using SM = D8Smem<DH, NT>;
   using CF = D8Cfg<NT>;
+  constexpr int kD8Stages = SM::kStages;
   constexpr int NC = DH / 16;                                      // 16-code chunks of a row
   constexpr int CT = CF::kWarps * 32;                              // consumer threads
   extern __shared__ uint8_t smem_raw[];
@@ -194,14 +196,14 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   const int g = lane >> 2, t4 = lane & 3;
   const int wq = warp;                                             // quarter of a page
   const int ctid = threadIdx.x;
-  // MMA row i (0..7) of a group of 8 keys is key krow(i): rows 4 apart sit in different halves of the banks
-  const int krow_g = ((g & 1) << 2) | (g >> 1);
-  const int l7 = lane & 7;
-  const int krow_l = ((l7 & 1) << 2) | (l7 >> 1);
+  // MMA row i (0..7) of a group of 8 keys is key krow(i), so that neighbouring rows of the K loads sit in different halves of
+  // the banks: rows of 128 bytes 4 apart, rows of 64 bytes next to each other
+  auto krow = [](int i) { return DH > 64 ? ((i & 1) << 2) | (i >> 1) : i; };
+  const int krow_g = krow(g), krow_l = krow(lane & 7);
   const uint32_t ring = smem_u32(smem);
-  const uint32_t k_off = uint32_t(wq * 16 + krow_g) * 128 + (((t4 ^ krow_g) & 7) << 4);          // chunk t4 of the lane's first key
+  const uint32_t k_off = c8_code_off<DH>(wq * 16 + krow_g, t4);    // chunk t4 of the lane's first key; chunk t4 + 4 is at ^ 64
   // ldmatrix: this lane's row and chunk (matrices 2 and 3 are the next chunk); chunk pair cp is at ^ (cp << 5)
-  const uint32_t v_off = uint32_t(SM::kTile) + uint32_t(wq * 16 + ((lane >> 3) & 1) * 8 + krow_l) * 128 + (((lane >> 4) ^ krow_l) << 4);
+  const uint32_t v_off = uint32_t(SM::kTile) + c8_code_off<DH>(wq * 16 + ((lane >> 3) & 1) * 8 + krow_l, lane >> 4);
   bool ok = true;
   int it = 0, st = 0;                                              // pages so far, their next stage and the parity of its phase
   uint32_t ph = 0;
@@ -294,7 +296,7 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
 #pragma unroll
         for (int hh = 0; hh < NC / 4; ++hh) {
-          const uint4 x = lds128(k_base ^ (hh << 6)), y = lds128((k_base + 8 * 128) ^ (hh << 6));
+          const uint4 x = lds128(k_base ^ (hh << 6)), y = lds128((k_base + SM::kTile / 8) ^ (hh << 6));       // (8 rows on)
           const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -360,7 +362,7 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         uint32_t keep0 = 0xffffffffu, keep1 = 0xffffffffu;
         if (tail) {
           const int i0 = t4 * 2, i1 = t4 * 2 + 1;                  // MMA key indices of this lane's halves
-          const int k0 = key0 + (((i0 & 1) << 2) | (i0 >> 1)), k1 = key0 + (((i1 & 1) << 2) | (i1 >> 1));
+          const int k0 = key0 + krow(i0), k1 = key0 + krow(i1);
           keep0 = (k0 < kv_len ? 0xffffu : 0u) | (k1 < kv_len ? 0xffff0000u : 0u);
           keep1 = (k0 + 8 < kv_len ? 0xffffu : 0u) | (k1 + 8 < kv_len ? 0xffff0000u : 0u);
         }

@@ -54,7 +54,7 @@ struct C8Smem {
   using CF = C8Cfg<EXPANDED>;
   static constexpr int kQTile = kC8Rows * DH * 2;
   static constexpr int kTile = kC8Keys * DH * 2;               // one fp16 operand tile
-  static constexpr int kRawTile = kC8Keys * 128;               // codes, rows padded to 128 bytes by the TMA box
+  static constexpr int kRawTile = c8_tile_bytes<DH>();         // codes
   static constexpr int kQOff = 0;
   static constexpr int kKOff = 2 * kQTile;
   static constexpr int kVOff = kKOff + CF::kRing * kTile;
@@ -353,7 +353,7 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 #pragma unroll 4
       for (int p = tid; p < kC8Keys * CH; p += 128) {
         const int row = p / CH, ch = p % CH;
-        uint4 x = *reinterpret_cast<const uint4*>(src + row * 128 + (((ch ^ row) & 7) << 4));
+        uint4 x = *reinterpret_cast<const uint4*>(src + c8_code_off<DH>(row, ch));
         if (row >= valid_rows) x = make_uint4(0, 0, 0, 0);
         uint4 u, v;
         c8_decode_natural<FMT>(x.x, u.x, u.y);
