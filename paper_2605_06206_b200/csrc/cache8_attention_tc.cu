@@ -182,6 +182,7 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     split = int(blockIdx.x) - d->first[lo];
     n_splits = d->first[lo + 1] - d->first[lo];
     per_split = d->per;
+    fence_proxy_async();                                   // (the copies that come here next go through the async proxy)
     __syncthreads();
   }
   int b, pair, q0;
@@ -193,15 +194,16 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   const bool bad = q_len < 0 || q_len > c.max_q_len || ctx < 0 || (long long)ctx + q_len > c.max_len;
   if (!bad && (q0 >= q_len || q_len < lc.min_q || q_len >= lc.end_q)) return;
   const int start = c8_block_prefix(c.q_lens, b, red);
-  if (bad || (long long)start + q_len > c.n_tokens) {     // lengths that disagree with what the host was told
+  const bool fits = !bad && (long long)start + q_len <= c.n_tokens;
+  const int tok0 = start + q0;
+  const int rows_here = min(kC8Rows, q_len - q0);
+  if (lc.split && split == 0 && threadIdx.x == 0) a.division[lin] = fits ? make_int4(int(blockIdx.x), n_splits, tok0, rows_here) : make_int4(0, 0, 0, 0);
+  if (!fits) {                                            // lengths that disagree with what the host was told
     if (threadIdx.x == 0) atomicExch(c.status, kStatusBounds);
     return;
   }
-  const int tok0 = start + q0;
-  const int rows_here = min(kC8Rows, q_len - q0);
   const int kv_len = ctx + q0 + rows_here;
   const int all_steps = (kv_len + kC8Keys - 1) / kC8Keys;
-  if (lc.split && split == 0 && threadIdx.x == 0) a.division[lin] = make_int4(int(blockIdx.x), n_splits, tok0, rows_here);
   const int step0 = split ? split * per_split : 0;
   const int n_steps = min(all_steps - step0, per_split);
 
@@ -659,7 +661,7 @@ cache8_join_kernel(const Cache8AttendArgs a, const C8Launch lc) {
   // (a block without tokens has left nothing)
   if (q_len < lc.min_q || q_len >= lc.end_q || q_len > c.max_q_len || ctx < 0 || (long long)ctx + q_len > c.max_len || q0 >= q_len) return;
   const int first = d.x, used = d.y, tok0 = d.z, rows_here = d.w;
-  if (used < 2 || (long long)tok0 - q0 + q_len > c.n_tokens) return;     // (one CTA: it has written the output itself)
+  if (used < 2) return;                                    // (one CTA: it has written the output itself; none: lengths that do not fit)
   for (int row = blockIdx.z * (kC8JoinThreads / 32) + warp; row < rows_here; row += gridDim.z * (kC8JoinThreads / 32)) {
     auto prow = [&](int s) { return (size_t(first + s) * 2 + t) * kC8Rows + row; };
     float m = -INFINITY;
@@ -698,8 +700,8 @@ cache8_join_kernel(const Cache8AttendArgs a, const C8Launch lc) {
 }
 
 // Codes of the pages of sequences [seq0, seq0 + n) -> operand tiles [sequence][page][n_kv][64][DH] (exact, unscaled; a
-// 96-wide head zero-padded) and their scales.  K becomes bf16, the type of the queries it meets, V fp16, the type of P.  One block per (page, KV head, K or V); rows behind the sequence's last
-// token become zeros.
+// 96-wide head zero-padded) and their scales.  K becomes bf16, the type of the queries it meets, V fp16, the type of P.  One
+// block per (page, KV head, K or V); rows behind the sequence's last token become zeros.
 constexpr int kC8ExpThreads = 128;
 template <int FMT, int DH>
 __global__ void __launch_bounds__(kC8ExpThreads)

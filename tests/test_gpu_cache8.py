@@ -684,6 +684,40 @@ def test_bad_lengths_and_pages_are_reported_and_skipped():
     assert s.ops.poll_status() == 0
 
 
+@pytest.mark.parametrize("q,tokens,longest", [([8, 8], 10, 8), ([2, 1], 2, 2), ([700, 700], 1000, 700), ([1, 1, 1], 2, 1)])
+def test_chunk_lengths_that_exceed_the_rows_of_the_call(q, tokens, longest):
+    """The sequence whose rows do not exist is skipped and reported; nothing is written behind the call's rows, also not by
+    a call that follows one with more rows."""
+    n = len(q)
+    s = Setup(8, 2, 64, "e4m3", [800] * n, seed=45, width=13)
+    s.fill([60] * n)
+    big = [max(x, 3) for x in q]
+    s.fill([60 + x for x in big])
+    wide = s.randn(sum(big), 8, 64).cuda()
+    s.ops.attend(wide, s.view([60] * n, big), max_q_len=max(big))   # more rows: what it leaves in the workspace fits them only
+    assert s.ops.poll_status() == 0
+    out = torch.full((sum(q) + 130, 8, 64), 5.0, dtype=torch.bfloat16, device="cuda")
+    x = s.randn(tokens, 8, 64)
+    w = torch.zeros(n, 2, s.width * PAGE, device="cuda")
+    s.ops.attend(x.cuda(), s.view([60] * n, q), out=out[:tokens], max_q_len=longest, weights_in=w, weights_out=w)
+    assert s.ops.poll_status() == -8
+    kp, vp = s.refs()
+    fit = [b for b in range(n) if sum(q[:b + 1]) <= tokens]
+    rows = sum(q[b] for b in fit)
+    o, mag, big_s, _ = ref.attend(kp, vp, s.table, [60] * len(fit), [q[b] for b in fit], x[:rows])
+    ref.check_attend(out[:rows], o, mag, big_s)
+    assert bool((out[tokens:] == 5.0).all())
+    k = s.randn(tokens, 2, 64)
+    before = s.refs()
+    s.ops.append(k.cuda(), k.cuda(), s.view([60] * n, q), max_q_len=longest)
+    assert s.ops.poll_status() == -8
+    kp, vp = before
+    for b in fit:
+        at = sum(q[:b])
+        kp.write(s.table[b], 60, k[at:at + q[b]].double()), vp.write(s.table[b], 60, k[at:at + q[b]].double())
+    s.same(kp, vp)
+
+
 def test_offsets_beyond_32_bits():
     """A pool of more than 4 GiB of K codes: the sequence's pages lie at its end."""
     n_kv, dh = 8, 128
