@@ -82,53 +82,82 @@ struct C8Launch {
 
 // A launch of fewer blocks than SMs gives every block as many CTAs as keep the longest of them short: `per` is the
 // smallest number of steps (at least kC8MinSteps) for which sum_i ceil(steps_i / per) CTAs fit the grid, and block i's
-// CTAs are first[i] .. first[i + 1] - 1.  Worked out by one warp of every CTA from the lengths on the device; a
-// block's first CTA leaves its part for the joining kernel (every block with a token has one).
+// CTAs are first[i] .. first[i + 1] - 1.  Worked out by every CTA from the lengths on the device, each of its warps trying
+// another `per` (a search by one warp took 2.4 us); a block's first CTA leaves its part for the joining kernel (every
+// block with a token has one).
 constexpr int kC8MaxSplitBlocks = 256, kC8MinSteps = 4;
-struct C8Division { int per, first[kC8MaxSplitBlocks + 1]; };
+struct C8Division { int per, lo, hi, fits[32], first[kC8MaxSplitBlocks + 1]; };
 __device__ __forceinline__ void c8_block_of(const Cache8Args& c, const C8Launch& lc, int pairs, int lin, int& b, int& pair, int& q0) {
   const int per_qb = pairs * lc.n_seqs;
   q0 = (lc.q_blocks - 1 - lin / per_qb) * kC8Rows;         // late query blocks (long causal extents) of the whole call first
   pair = (lin % per_qb) % pairs;
   b = lc.seq0 + (lin % per_qb) / pairs;
 }
+// ceil(a / b) for 0 <= a < 2^24, 0 < b: a rounded quotient and one correction either way (an integer division takes several
+// times as long, and the search below makes dozens)
+__device__ __forceinline__ int c8_ceil_div(int a, int b, float inv_b) {
+  int n = __float2int_ru(float(a) * inv_b);
+  n += n * b < a ? 1 : 0;
+  n -= (n - 1) * b >= a ? 1 : 0;
+  return n;
+}
 __device__ __forceinline__ void c8_divide(const Cache8Args& c, const C8Launch& lc, int pairs, int n_blocks, int n_ctas, C8Division* d) {
-  const int lane = threadIdx.x & 31;
-  int most = 0;
-  for (int i = lane; i < n_blocks; i += 32) {
-    int b, pair, q0, steps = 0;
-    c8_block_of(c, lc, pairs, i, b, pair, q0);
-    const int q_len = c.q_lens[b], ctx = c.context_lens[b];
-    const bool bad = q_len < 0 || q_len > c.max_q_len || ctx < 0 || (long long)ctx + q_len > c.max_len;
-    if (bad && blockIdx.x == 0) atomicExch(c.status, kStatusBounds);
-    if (!bad && q_len >= lc.min_q && q_len < lc.end_q && q0 < q_len)
-      steps = (ctx + min(q0 + kC8Rows, q_len) + kC8Keys - 1) / kC8Keys;
-    d->first[i] = steps;
-    most = max(most, steps);
-  }
-  __syncwarp();
-  most = __reduce_max_sync(0xffffffffu, most);
-  int lo = kC8MinSteps, hi = max(most, kC8MinSteps);       // smallest `per` in [lo, hi] that fits (hi does: one CTA a block)
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    int n = 0;
-    for (int i = lane; i < n_blocks; i += 32) n += (d->first[i] + mid - 1) / mid;
-    if (__reduce_add_sync(0xffffffffu, n) <= n_ctas) hi = mid; else lo = mid + 1;
-  }
-  int base = 0;
-  for (int i0 = 0; i0 < n_blocks; i0 += 32) {
-    const int n = i0 + lane < n_blocks ? (d->first[i0 + lane] + lo - 1) / lo : 0;
-    int incl = n;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += v;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n_warps = blockDim.x >> 5;
+  if (warp == 0) {
+    int most = 0, total = 0;
+    for (int i = lane; i < n_blocks; i += 32) {
+      int b, pair, q0, steps = 0;
+      c8_block_of(c, lc, pairs, i, b, pair, q0);
+      const int q_len = c.q_lens[b], ctx = c.context_lens[b];
+      const bool bad = q_len < 0 || q_len > c.max_q_len || ctx < 0 || (long long)ctx + q_len > c.max_len;
+      if (bad && blockIdx.x == 0) atomicExch(c.status, kStatusBounds);
+      if (!bad && q_len >= lc.min_q && q_len < lc.end_q && q0 < q_len)
+        steps = (ctx + min(q0 + kC8Rows, q_len) + kC8Keys - 1) / kC8Keys;
+      d->first[i] = steps;
+      most = max(most, steps);
+      total += steps;
     }
-    __syncwarp();
-    if (i0 + lane < n_blocks) d->first[i0 + lane] = base + incl - n;
-    base += __shfl_sync(0xffffffffu, incl, 31);
+    most = __reduce_max_sync(0xffffffffu, most);
+    total = __reduce_add_sync(0xffffffffu, total);
+    // the answer is in [lo, hi]: hi fits (one CTA a block), less than an even share does not
+    if (lane == 0) { d->lo = max(kC8MinSteps, total / n_ctas); d->hi = max(most, max(kC8MinSteps, total / n_ctas)); }
   }
-  if (lane == 0) { d->first[n_blocks] = base; d->per = lo; }
+  __syncthreads();
+  int lo = d->lo, hi = d->hi;
+  while (lo < hi) {                                        // (the same in every thread)
+    const int stride = (hi - lo + n_warps - 1) / n_warps;
+    const int mine = min(lo + warp * stride, hi);
+    const float inv = 1.f / float(mine);
+    int n = 0;
+    for (int i = lane; i < n_blocks; i += 32) n += c8_ceil_div(d->first[i], mine, inv);
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (lane == 0) d->fits[warp] = n <= n_ctas;
+    __syncthreads();
+    const uint32_t ok = __ballot_sync(0xffffffffu, lane < n_warps && d->fits[lane]);
+    const int w = ok ? __ffs(ok) - 1 : n_warps;            // the first that fits; the one before it does not
+    const int new_hi = w < n_warps ? min(lo + w * stride, hi) : hi;
+    lo = w > 0 ? min(lo + (w - 1) * stride + 1, new_hi) : lo;
+    hi = w > 0 ? new_hi : lo;
+    __syncthreads();
+  }
+  if (warp == 0) {
+    int base = 0;
+    const float inv = 1.f / float(lo);
+    for (int i0 = 0; i0 < n_blocks; i0 += 32) {
+      const int n = i0 + lane < n_blocks ? c8_ceil_div(d->first[i0 + lane], lo, inv) : 0;
+      int incl = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+      }
+      __syncwarp();
+      if (i0 + lane < n_blocks) d->first[i0 + lane] = base + incl - n;
+      base += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    if (lane == 0) { d->first[n_blocks] = base; d->per = lo; }
+  }
+  __syncthreads();
 }
 
 template <int FMT, int DH, bool EXPANDED>
@@ -170,8 +199,7 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   int lin = blockIdx.x, split = 0, n_splits = 1, per_split = 0x7fffffff;
   if (lc.split) {
     C8Division* d = reinterpret_cast<C8Division*>(smem);   // (before the tiles)
-    if (warp == 0) c8_divide(c, lc, pairs, n_blocks, gridDim.x, d);
-    __syncthreads();
+    c8_divide(c, lc, pairs, n_blocks, gridDim.x, d);
     if (int(blockIdx.x) >= d->first[n_blocks]) return;
     int lo = 0, hi = n_blocks - 1;                         // the last block whose first CTA is not behind this one
     while (lo < hi) {
