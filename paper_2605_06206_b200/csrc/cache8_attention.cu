@@ -27,6 +27,8 @@
 // six stages took 114 and 60 us: more copies in flight than about 144 KB an SM slow the memory down.
 #include <math.h>
 
+#include <type_traits>
+
 #include "cache8.cuh"
 #include "cache8.h"
 #include "decode_walk.cuh"
@@ -36,6 +38,7 @@ namespace foe {
 template <int DH> constexpr int d8_stages() { return DH > 64 ? 3 : 6; }      // about 48 KB in flight
 constexpr int kD8MinTiles = 2;                   // fewest pages per CTA
 constexpr int kD8Gap = 6;                        // what starting a pair costs, in pages (decode_walk.cuh)
+constexpr int kD8Parts = 80;                     // a pair is cut into about this many segments at most: one CTA merges them, 16 in 0.8 us
 constexpr float kD8Shift = 6.f;                  // P' = 2^(t - m + shift)
 constexpr float kD8Lazy = 8.f;                   // the reference maximum moves when a score exceeds it by more than this
 
@@ -122,7 +125,7 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   }
 
   DcWalk w;
-  if (!dc_begin<kD8Gap, true>(c, kD8MinTiles, w)) return;                // (the same in every warp)
+  if (!dc_begin<kD8Gap, true, kD8Parts>(c, kD8MinTiles, w)) return;                // (the same in every warp)
 
   if (warp == CF::kWarps) {
     // ------------------------------------------------------------------ producer
@@ -497,41 +500,50 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         for (int s = lane; s < n_segs; s += 32) m = fmaxf(m, __ldcg(a.part_ml + (slot_of(s) * 16 + r) * 2));
 #pragma unroll
         for (int o2 = 16; o2 > 0; o2 >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o2));
-        float acc[DH / 32];
+        // (a lane takes DH / 32 neighbouring columns: one load a segment; behind the last segment that one again, with
+        //  factor 0, so that the loads of a batch go out together)
+        typedef typename std::conditional<DH == 128, float4, float2>::type Vec;
+        constexpr int W = DH / 32;
+        float acc[W];
 #pragma unroll
-        for (int i = 0; i < DH / 32; ++i) acc[i] = 0.f;
+        for (int i = 0; i < W; ++i) acc[i] = 0.f;
         float l = 0.f;
-        for (int c0 = 0; c0 < n_segs; c0 += 32) {
-          const int n = min(32, n_segs - c0);
-          float fs = 0.f, ls = 0.f;                                // lane s: factor and row sum of segment c0 + s
-          if (lane < n) {
-            const float ms = __ldcg(a.part_ml + (slot_of(c0 + lane) * 16 + r) * 2);
-            fs = ms == -INFINITY ? 0.f : fast_exp2(ms - m);
-            ls = __ldcg(a.part_ml + (slot_of(c0 + lane) * 16 + r) * 2 + 1);
-          }
-          for (int u0 = 0; u0 < n; u0 += 8) {
-            float v[8][DH / 32];
+        auto add = [&](auto ahead) {
+          constexpr int AHEAD = decltype(ahead)::value;
+          for (int c0 = 0; c0 < n_segs; c0 += 32) {
+            const int n = min(32, n_segs - c0);
+            float fs = 0.f, ls = 0.f;                              // lane s: factor and row sum of segment c0 + s
+            if (lane < n) {
+              const float ms = __ldcg(a.part_ml + (slot_of(c0 + lane) * 16 + r) * 2);
+              fs = ms == -INFINITY ? 0.f : fast_exp2(ms - m);
+              ls = __ldcg(a.part_ml + (slot_of(c0 + lane) * 16 + r) * 2 + 1);
+            }
+            for (int u0 = 0; u0 < n; u0 += AHEAD) {
+              Vec v[AHEAD];
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
+              for (int u = 0; u < AHEAD; ++u)
+                v[u] = __ldcg(reinterpret_cast<const Vec*>(a.part_o + (slot_of(c0 + min(u0 + u, n - 1)) * 16 + r) * DH) + lane);
 #pragma unroll
-              for (int i = 0; i < DH / 32; ++i)
-                v[u][i] = u0 + u < n ? __ldcg(a.part_o + (slot_of(c0 + u0 + u) * 16 + r) * DH + i * 32 + lane) : 0.f;
+              for (int u = 0; u < AHEAD; ++u) {
+                const float fu = __shfl_sync(0xffffffffu, fs, (u0 + u) & 31);   // (0 behind the last segment)
+                const float lu = __shfl_sync(0xffffffffu, ls, (u0 + u) & 31);
+                l += fu * lu;
+                const float* f = reinterpret_cast<const float*>(&v[u]);
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-              const float fu = __shfl_sync(0xffffffffu, fs, (u0 + u) & 31);   // (0 past the last segment)
-              const float lu = __shfl_sync(0xffffffffu, ls, (u0 + u) & 31);
-              l += fu * lu;
-#pragma unroll
-              for (int i = 0; i < DH / 32; ++i) acc[i] += fu * v[u][i];
+                for (int i = 0; i < W; ++i) acc[i] += fu * f[i];
+              }
             }
           }
-        }
+        };
+        if (n_segs <= 8) add(std::integral_constant<int, 8>());
+        else add(std::integral_constant<int, 16>());
         const float inv = 1.f / l;
         if (tok >= c.n_tokens) continue;
         __nv_bfloat16* dst = a.out + (long long)tok * a.out_stride + (kvh * G + r) * c.dh;
+        if (lane * W < c.dh) {                                     // (dh is a multiple of W)
 #pragma unroll
-        for (int i = 0; i < DH / 32; ++i)
-          if (i * 32 + lane < c.dh) dst[i * 32 + lane] = __float2bfloat16_rn(acc[i] * inv);
+          for (int i = 0; i < W; i += 2) *reinterpret_cast<uint32_t*>(dst + lane * W + i) = pack_bf16(acc[i] * inv, acc[i + 1] * inv);
+        }
         if (lane == 0 && a.lse) a.lse[size_t(tok) * c.n_q + kvh * G + r] = m - kD8Shift + log2f(l);
       }
     }

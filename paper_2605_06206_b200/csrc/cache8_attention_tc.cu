@@ -692,15 +692,8 @@ cache8_join_kernel(const Cache8AttendArgs a, const C8Launch lc) {
   if (used < 2) return;                                    // (one CTA: it has written the output itself; none: lengths that do not fit)
   for (int row = blockIdx.z * (kC8JoinThreads / 32) + warp; row < rows_here; row += gridDim.z * (kC8JoinThreads / 32)) {
     auto prow = [&](int s) { return (size_t(first + s) * 2 + t) * kC8Rows + row; };
-    float m = -INFINITY;
-    for (int s = lane; s < used; s += 32) m = fmaxf(m, a.part_ml[prow(s) * 2]);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    float acc[DH / 32], l = 0.f;
-#pragma unroll
-    for (int q = 0; q < DH / 32; ++q) acc[q] = 0.f;
-    for (int s0 = 0; s0 < used; s0 += 4) {                 // four splits' loads in flight
-      float ms[4], ls[4], v[4][DH / 32];
+    float ms[4], ls[4], v[4][DH / 32];
+    auto load = [&](int s0) {                              // four splits' loads in flight
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const size_t p = prow(min(s0 + u, used - 1));
@@ -709,6 +702,17 @@ cache8_join_kernel(const Cache8AttendArgs a, const C8Launch lc) {
 #pragma unroll
         for (int q = 0; q < DH / 32; ++q) v[u][q] = a.part_o[p * DH + q * 32 + lane];
       }
+    };
+    load(0);                                               // (beside the maximum's)
+    float m = -INFINITY;
+    for (int s = lane; s < used; s += 32) m = fmaxf(m, a.part_ml[prow(s) * 2]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    float acc[DH / 32], l = 0.f;
+#pragma unroll
+    for (int q = 0; q < DH / 32; ++q) acc[q] = 0.f;
+    for (int s0 = 0; s0 < used; s0 += 4) {
+      if (s0 > 0) load(s0);
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         if (s0 + u >= used) break;
@@ -814,13 +818,14 @@ static int launch_chunk_t(const CUtensorMap& tmQ, const CUtensorMap& tmK, const 
   const long long page_reads = (long long)((c.max_q_len + kC8Rows - 1) / kC8Rows) * (c.n_q / tiles) * c.n_seqs * c.max_kv_pages;
   const bool expand = c.max_q_len >= cache8_expand_min_tokens(G, c.dh) && page_reads >= 16LL * n_sms;
   const int long_q = (cache8_expand_min_tokens(G, c.dh) + 7) / 8;        // chunks from here on run on expanded tiles, if any (at least 6)
-  // query blocks of a launch over n sequences of up to `longest` tokens; one CTA per SM, so a launch of fewer blocks
-  // than that splits their keys.  Returns the CTAs.
+  // query blocks of a launch over n sequences of up to `longest` tokens.  One CTA per SM, so a launch of fewer blocks than
+  // that splits their keys where the sequences can be long enough: dividing and joining cost 8 to 10 us, a step 1, and where
+  // the blocks fill more than half of the SMs only uneven lengths leave something to gain.  Returns the CTAs.
   auto plan = [&](C8Launch& lc, int longest, int n) {
     lc.q_blocks = (longest + kC8Rows - 1) / kC8Rows;
     lc.n_seqs = n;
     const long long blocks = (long long)lc.q_blocks * (c.n_q / tiles) * n;
-    lc.split = blocks < n_sms && blocks <= kC8MaxSplitBlocks && c.max_kv_pages > kC8MinSteps;
+    lc.split = blocks < n_sms && blocks <= kC8MaxSplitBlocks && c.max_kv_pages >= (2 * blocks <= n_sms ? 16 : 48);
     return unsigned(lc.split ? n_sms : blocks);
   };
   auto join = [&](const C8Launch& lc, int longest) {

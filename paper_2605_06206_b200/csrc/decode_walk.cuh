@@ -2,6 +2,7 @@
 // pairs form one list (sequence-major, then KV head, then page) of T entries and CTA c takes the entries
 // [c * per, (c + 1) * per), per = max(min_tiles, ceil(T / grid)).  GAP: entries without a page in front of every pair,
 // which stand for the time that starting a pair costs, so that a CTA whose range holds more pairs gets fewer pages.
+// PARTS > 0: per is also at least a PARTS-th of the longest pair, which bounds the segments that one CTA has to merge.
 // SINGLES: where the call gives q_lens, only the sequences with one new token count (the others have no entries).
 // Args: context_lens, n_seqs, n_kv, max_kv_pages (SINGLES: q_lens, or nullptr).
 #pragma once
@@ -30,7 +31,7 @@ __device__ __forceinline__ int dc_pages(const Args& a, int b, int* kv_len) {
 }
 
 // Every warp works this out for itself (all 32 lanes): the CTA's range and where it starts.  False: nothing to do.
-template <int GAP = 0, bool SINGLES = false, typename Args>
+template <int GAP = 0, bool SINGLES = false, int PARTS = 0, typename Args>
 __device__ __forceinline__ bool dc_begin(const Args& a, int min_tiles, DcWalk& w) {
   const int lane = threadIdx.x & 31;
   // a lane takes `share` consecutive sequences: one pass for their entries, one scan over the lanes, and the lane whose
@@ -38,10 +39,12 @@ __device__ __forceinline__ bool dc_begin(const Args& a, int min_tiles, DcWalk& w
   const int share = (a.n_seqs + 31) >> 5;
   const int b_lo = min(lane * share, a.n_seqs), b_hi = min(b_lo + share, a.n_seqs);
   int mine = 0, kl = 0, np = 0;                  // (with up to 32 sequences kl and np are the lane's one)
+  int longest = 0;
 #pragma unroll 4                                   // (the lengths' loads in flight together)
   for (int b = b_lo; b < b_hi; ++b) {
     np = dc_pages<SINGLES>(a, b, &kl);
     mine += np + (np > 0 ? GAP : 0);
+    longest = max(longest, np);
   }
   int incl = mine;
 #pragma unroll
@@ -51,6 +54,7 @@ __device__ __forceinline__ bool dc_begin(const Args& a, int min_tiles, DcWalk& w
   }
   const int T = __shfl_sync(0xffffffffu, incl, 31) * a.n_kv;
   w.per = max(min_tiles, (T + int(gridDim.x) - 1) / int(gridDim.x));
+  if constexpr (PARTS > 0) w.per = max(w.per, (__reduce_max_sync(0xffffffffu, longest) + PARTS - 1) / PARTS);
   const long long t0 = (long long)blockIdx.x * w.per;
   if (t0 >= T) return false;
   w.t = int(t0);
