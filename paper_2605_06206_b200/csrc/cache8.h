@@ -18,6 +18,7 @@ struct Cache8Args {
   const int* q_lens;                // [n_seqs] new tokens, or nullptr: one each
   int n_seqs, max_pages_per_seq, num_pages, n_tokens, max_q_len;
   int n_q, n_kv, dh;
+  int few_q;                        // sequences of up to this many new tokens go the way of single tokens
   int max_len;                      // tokens a sequence may reach: min(64 * table width, the handle's max_context)
   int max_kv_pages;                 // pages of that many tokens
   int* status;
@@ -73,7 +74,7 @@ struct Cache8EvictArgs {
 
 // fmt: kC8E4M3 or kC8Int8 (cache8.cuh)
 void launch_cache8_append(int fmt, const Cache8AppendArgs& a, cudaStream_t st);
-// single tokens: q_lens nullptr, or the sequences with q_lens == 1
+// single tokens: q_lens nullptr, or the sequences with 1 <= q_lens <= few_q
 void launch_cache8_decode(int fmt, const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a, int n_sms,
                           cudaStream_t st);
 size_t cache8_decode_part_rows(int n_sms);   // rows of part_o / part_ml

@@ -152,6 +152,9 @@ Cache8Args cache8_args(const foe_cache* h, const foe_cache_view* v, int* status)
   const long long table = (long long)v->max_pages_per_seq * 64;
   c.max_len = int(table < h->cfg.max_context ? table : h->cfg.max_context);
   c.max_kv_pages = (c.max_len + 63) / 64;
+  // (query, head) rows of a KV head are the columns of the single-token kernel's products, 8 of them in a tile
+  const int group = c.n_q / c.n_kv;
+  c.few_q = group >= 8 ? 1 : 8 / group;
   c.status = status;
   return c;
 }
@@ -175,17 +178,18 @@ int cache8_attend(foe_cache* h, const foe_cache_view* v, const void* q, long lon
   } else {
     CUtensorMap tmQ = tmK;                       // (only long chunks read their queries through a map)
     if (h->ws.pages && a.c.n_tokens > 0 && !make_query_map(&tmQ, q, a.c.n_tokens, a.c.n_q, a.c.dh, q_stride, q_head_stride)) return -1;
-    // Sequences with one new token go the way of single tokens: a tile of 128 query rows would read their cache at a
-    // fraction of the memory's rate.  (No sequence has fewer tokens than those that the others, at max_q_len each, leave.)
-    const bool singles = a.c.n_tokens - (long long)(a.c.n_seqs - 1) * a.c.max_q_len < 2;
+    // Sequences with a few new tokens go the way of single tokens: a tile of 128 query rows would read their cache at a
+    // fraction of the memory's rate (16 query heads on 4 of 128; us as chunks / here: 2 new tokens at 16 x 8000 cached tokens
+    // 169 / 36, at 64 x 4000 340 / 58, at 64 x 500 69 / 22, at 1 x 8000 24.5 / 16.8).  (No sequence has fewer tokens than those that the others, at max_q_len each, leave.)
+    const bool few = a.c.n_tokens - (long long)(a.c.n_seqs - 1) * a.c.max_q_len <= a.c.few_q;
     n = 0;
-    if (singles && a.c.n_tokens > 0) {
+    if (few && a.c.n_tokens > 0) {
       Cache8AttendArgs one = a;
       one.logits = nullptr;
       launch_cache8_decode(h->cfg.format, tmK, tmV, one, h->n_sms, st);
       n = 1;
     }
-    if (a.c.max_q_len > 1 || !singles) n += launch_cache8_chunk(h->cfg.format, tmQ, tmK, tmV, a, h->ws, singles ? 2 : 0, h->n_sms, st);
+    if (a.c.max_q_len > a.c.few_q || !few) n += launch_cache8_chunk(h->cfg.format, tmQ, tmK, tmV, a, h->ws, few ? a.c.few_q + 1 : 0, h->n_sms, st);
   }
   if (w_out) {
     Cache8WeightsArgs w;

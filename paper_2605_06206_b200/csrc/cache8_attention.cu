@@ -1,4 +1,5 @@
-// Attention of single new tokens over the 8-bit cache (in a call of chunks: of its sequences with one new token).
+// Attention of single new tokens over the 8-bit cache (in a call of chunks: of its sequences with up to few_q new tokens,
+// whose (query, head) rows of a KV head fit one tile of 8).
 //
 // Decode reads every code of the cache once: 1 byte per K and V element, so the kernel has half the time per element of
 // a bf16 one and its arithmetic has to be lean.
@@ -110,7 +111,7 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   pdl_wait();
   pdl_launch_dependents();
 
-  // A call with q_lens runs its sequences of one new token here and the others as chunks; their lengths are looked over once.
+  // A call with q_lens runs its sequences of few new tokens here and the others as chunks; their lengths are looked over once.
   if (c.q_lens && blockIdx.x == 0 && warp == 0) {
     long long sum = 0;
     bool bad = false;
@@ -211,7 +212,7 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   int it = 0, st = 0;                                              // pages so far, their next stage and the parity of its phase
   uint32_t ph = 0;
   // pairs whose keys are split over CTAs: at most the CTA's first and its last; their tickets are taken at the end
-  int pend_b[2], pend_kvh[2], pend_c0[2], pend_n[2], pend_tok[2], n_pend = 0;
+  int pend_b[2], pend_kvh[2], pend_c0[2], pend_n[2], pend_tok[2], pend_rows[2], n_pend = 0;
 
   while (w.t < w.t_end) {
     const int len = dc_segment_len(w);
@@ -220,13 +221,16 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     const int c_first = pair_first / w.per;
     const int n_segs = (pair_first + w.np - 1) / w.per - c_first + 1;
     const int seg = int(blockIdx.x) - c_first;
-    int tok = b;                                                   // row of the sequence's token
+    int tok = b, nq = 1;                                           // row of the sequence's first new token, new tokens
     if (c.q_lens) {
       int before = 0;
       for (int i = lane; i < b; i += 32) before += max(c.q_lens[i], 0);
       tok = __reduce_add_sync(0xffffffffu, before);
+      nq = c.q_lens[b];
     }
-    const bool tok_ok = tok < c.n_tokens;                          // (lengths that do not add up are reported above)
+    const bool tok_ok = tok + nq <= c.n_tokens;                    // (lengths that do not add up are reported above)
+    const int rows = G * nq;                                       // columns of the products: row r is query r / G, head r % G
+    const int lim0 = kv_len - nq + 1;                              // query i sees the keys before lim0 + i
     if (w.page == 0 && kvh == 0 && ctid == 0) {
       const int ctx = c.context_lens[b];
       if (ctx < 0 || ctx >= c.max_len) atomicExch(c.status, kStatusBounds);
@@ -243,8 +247,9 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       for (int hh = 0; hh < NC / 4; ++hh) {
         const int d0 = (t4 + 4 * hh) * 16;
         v[hh][0] = v[hh][1] = make_uint4(0, 0, 0, 0);
-        if (n * 8 + g < G && d0 < c.dh && tok_ok) {
-          const uint4* p = reinterpret_cast<const uint4*>(a.q + (long long)tok * a.q_stride + (kvh * G + n * 8 + g) * a.q_head_stride + d0);
+        if (n * 8 + g < rows && d0 < c.dh && tok_ok) {
+          const int i = nq == 1 ? 0 : (n * 8 + g) / G, hd = n * 8 + g - i * G;
+          const uint4* p = reinterpret_cast<const uint4*>(a.q + (long long)(tok + i) * a.q_stride + (kvh * G + hd) * a.q_head_stride + d0);
           v[hh][0] = __ldg(p);
           v[hh][1] = __ldg(p + 1);
         }
@@ -310,7 +315,7 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
             for (int n = 0; n < NT; ++n) mma_f16_16816(s[n], a0, a1, a2, a3, qf[n][hh * 4 + i][0], qf[n][hh * 4 + i][1]);
           }
         }
-        const bool tail = key0 + 16 > kv_len;
+        const bool tail = key0 + 16 > lim0;                        // some row does not see some key
         bool grow = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -327,8 +332,12 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
           s[n][2] = fmaf(s[n][2], f0, sc.y);
           s[n][3] = fmaf(s[n][3], f1, sc.y);
           if (tail) {
-            if (key0 + krow_g >= kv_len) s[n][0] = s[n][1] = -INFINITY;
-            if (key0 + krow_g + 8 >= kv_len) s[n][2] = s[n][3] = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {                          // first key that row 2 t4 + e does not see
+              const int lim = nq == 1 ? kv_len : min(lim0 + (n * 8 + t4 * 2 + e) / G, kv_len);
+              if (key0 + krow_g >= lim) s[n][e] = -INFINITY;
+              if (key0 + krow_g + 8 >= lim) s[n][e + 2] = -INFINITY;
+            }
           }
           grow = grow || fmaxf(s[n][0], s[n][2]) > m_ref[n][0] + kD8Lazy || fmaxf(s[n][1], s[n][3]) > m_ref[n][1] + kD8Lazy;
         }
@@ -454,23 +463,24 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     const int d = ctid % DH;
     if (n_segs == 1) {
       // the whole pair was this segment: normalise and store
-      for (int r = ctid / DH; ok && r < G; r += CT / DH) {
-        if (d < c.dh && tok_ok)                                    // (a 96-wide head is computed zero-padded to 128)
-          a.out[(long long)tok * a.out_stride + (kvh * G + r) * c.dh + d] = __float2bfloat16_rn(mo[r * SM::kPitch + d] * (1.f / row_l[r]));
-        if (d == 0 && a.lse && tok_ok) a.lse[size_t(tok) * c.n_q + kvh * G + r] = row_m[r] - kD8Shift + log2f(row_l[r]);
+      for (int r = ctid / DH; ok && tok_ok && r < rows; r += CT / DH) {
+        const int i = nq == 1 ? 0 : r / G, hd = kvh * G + r - i * G;
+        if (d < c.dh)                                              // (a 96-wide head is computed zero-padded to 128)
+          a.out[(long long)(tok + i) * a.out_stride + hd * c.dh + d] = __float2bfloat16_rn(mo[r * SM::kPitch + d] * (1.f / row_l[r]));
+        if (d == 0 && a.lse) a.lse[size_t(tok + i) * c.n_q + hd] = row_m[r] - kD8Shift + log2f(row_l[r]);
       }
     } else {
       // A segment whose wait ran out writes no partial state but still takes its ticket: the counter of its pair
       // returns to zero and the handle stays usable (this call's output is not; the status word says so).
       const size_t slot = size_t(blockIdx.x) * 2 + (seg == 0 ? 1 : 0);
-      for (int r = ctid / DH; ok && r < G; r += CT / DH) {
+      for (int r = ctid / DH; ok && r < rows; r += CT / DH) {
         a.part_o[(slot * 16 + r) * DH + d] = mo[r * SM::kPitch + d];
         if (d == 0) {
           a.part_ml[(slot * 16 + r) * 2] = row_m[r];
           a.part_ml[(slot * 16 + r) * 2 + 1] = row_l[r];
         }
       }
-      pend_b[n_pend & 1] = b; pend_kvh[n_pend & 1] = kvh; pend_c0[n_pend & 1] = c_first; pend_n[n_pend & 1] = n_segs; pend_tok[n_pend & 1] = tok;
+      pend_b[n_pend & 1] = b; pend_kvh[n_pend & 1] = kvh; pend_c0[n_pend & 1] = c_first; pend_n[n_pend & 1] = n_segs; pend_tok[n_pend & 1] = tok; pend_rows[n_pend & 1] = tok_ok ? rows : 0;
       ++n_pend;
     }
     d8_bar<CT>();                                                  // mo and mm are free for the next segment
@@ -487,15 +497,16 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     }
     d8_bar<CT>();
     for (int q = 0; q < n_pend; ++q) {
-      const int b = pend_b[q], kvh = pend_kvh[q], c_first = pend_c0[q], n_segs = pend_n[q], tok = pend_tok[q];
+      const int b = pend_b[q], kvh = pend_kvh[q], c_first = pend_c0[q], n_segs = pend_n[q], tok = pend_tok[q], rows = pend_rows[q];
       if (ticket_s[q] != n_segs - 1) continue;
       if (ctid == 0) a.split_done[b * c.n_kv + kvh] = 0;           // re-armed for the next call
       __threadfence();
-      // One warp per query head.  The segments' (m, l) are read one per lane and their outputs eight segments at a
+      // One warp per row.  The segments' (m, l) are read one per lane and their outputs eight segments at a
       // time; the sums run in segment order.  Segment s lives in slot 1 of CTA c_first (s = 0) or slot 0 of CTA
       // c_first + s.
       auto slot_of = [&](int s) { return s == 0 ? size_t(c_first) * 2 + 1 : size_t(c_first + s) * 2; };
-      for (int r = warp; r < G; r += CF::kWarps) {
+      for (int r = warp; r < rows; r += CF::kWarps) {
+        const int i = rows == G ? 0 : r / G, hd = kvh * G + r - i * G, t = tok + i;
         float m = -INFINITY;
         for (int s = lane; s < n_segs; s += 32) m = fmaxf(m, __ldcg(a.part_ml + (slot_of(s) * 16 + r) * 2));
 #pragma unroll
@@ -538,13 +549,12 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         if (n_segs <= 8) add(std::integral_constant<int, 8>());
         else add(std::integral_constant<int, 16>());
         const float inv = 1.f / l;
-        if (tok >= c.n_tokens) continue;
-        __nv_bfloat16* dst = a.out + (long long)tok * a.out_stride + (kvh * G + r) * c.dh;
+        __nv_bfloat16* dst = a.out + (long long)t * a.out_stride + hd * c.dh;
         if (lane * W < c.dh) {                                     // (dh is a multiple of W)
 #pragma unroll
           for (int i = 0; i < W; i += 2) *reinterpret_cast<uint32_t*>(dst + lane * W + i) = pack_bf16(acc[i] * inv, acc[i + 1] * inv);
         }
-        if (lane == 0 && a.lse) a.lse[size_t(tok) * c.n_q + kvh * G + r] = m - kD8Shift + log2f(l);
+        if (lane == 0 && a.lse) a.lse[size_t(t) * c.n_q + hd] = m - kD8Shift + log2f(l);
       }
     }
   }

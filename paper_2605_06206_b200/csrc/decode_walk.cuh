@@ -3,8 +3,8 @@
 // [c * per, (c + 1) * per), per = max(min_tiles, ceil(T / grid)).  GAP: entries without a page in front of every pair,
 // which stand for the time that starting a pair costs, so that a CTA whose range holds more pairs gets fewer pages.
 // PARTS > 0: per is also at least a PARTS-th of the longest pair, which bounds the segments that one CTA has to merge.
-// SINGLES: where the call gives q_lens, only the sequences with one new token count (the others have no entries).
-// Args: context_lens, n_seqs, n_kv, max_kv_pages (SINGLES: q_lens, or nullptr).
+// FEW: where the call gives q_lens, only the sequences with 1 to few_q new tokens count (the others have no entries).
+// Args: context_lens, n_seqs, n_kv, max_kv_pages (FEW: q_lens, or nullptr, and few_q).
 #pragma once
 
 #include "common.cuh"
@@ -20,10 +20,15 @@ struct DcWalk {
   int per;
 };
 
-template <bool SINGLES = false, typename Args>
+template <bool FEW = false, typename Args>
 __device__ __forceinline__ int dc_pages(const Args& a, int b, int* kv_len) {
-  if constexpr (SINGLES) {
-    if (a.q_lens && a.q_lens[b] != 1) { *kv_len = 0; return 0; }
+  if constexpr (FEW) {
+    if (a.q_lens) {
+      const int n = a.q_lens[b];
+      if (n < 1 || n > a.few_q) { *kv_len = 0; return 0; }
+      *kv_len = min(max(a.context_lens[b], 0) + n, a.max_kv_pages * 64);      // cached tokens + the new ones
+      return (*kv_len + 63) >> 6;
+    }
   }
   const int ctx = min(max(a.context_lens[b], 0), a.max_kv_pages * 64 - 1);   // (out-of-range values are reported by the QKV step)
   *kv_len = ctx + 1;                                                          // cached tokens + the new one
@@ -31,7 +36,7 @@ __device__ __forceinline__ int dc_pages(const Args& a, int b, int* kv_len) {
 }
 
 // Every warp works this out for itself (all 32 lanes): the CTA's range and where it starts.  False: nothing to do.
-template <int GAP = 0, bool SINGLES = false, int PARTS = 0, typename Args>
+template <int GAP = 0, bool FEW = false, int PARTS = 0, typename Args>
 __device__ __forceinline__ bool dc_begin(const Args& a, int min_tiles, DcWalk& w) {
   const int lane = threadIdx.x & 31;
   // a lane takes `share` consecutive sequences: one pass for their entries, one scan over the lanes, and the lane whose
@@ -42,7 +47,7 @@ __device__ __forceinline__ bool dc_begin(const Args& a, int min_tiles, DcWalk& w
   int longest = 0;
 #pragma unroll 4                                   // (the lengths' loads in flight together)
   for (int b = b_lo; b < b_hi; ++b) {
-    np = dc_pages<SINGLES>(a, b, &kl);
+    np = dc_pages<FEW>(a, b, &kl);
     mine += np + (np > 0 ? GAP : 0);
     longest = max(longest, np);
   }
@@ -63,7 +68,7 @@ __device__ __forceinline__ bool dc_begin(const Args& a, int min_tiles, DcWalk& w
   const bool hit = mine > 0 && w.t >= first && w.t < first + a.n_kv * mine;
   if (hit && share > 1) {
     for (;; ++b) {
-      np = dc_pages<SINGLES>(a, b, &kl);
+      np = dc_pages<FEW>(a, b, &kl);
       const int size = a.n_kv * (np + (np > 0 ? GAP : 0));
       if (w.t < first + size) break;             // (before b_hi: the lane's entries hold w.t)
       first += size;
@@ -91,7 +96,7 @@ __device__ __forceinline__ int dc_segment_len(const DcWalk& w) { return min(w.np
 template <int GAP = 0>
 __device__ __forceinline__ int dc_pair_first(const DcWalk& w) { return w.seq_first + w.kvh * (w.np + GAP) + GAP; }
 
-template <int GAP = 0, bool SINGLES = false, typename Args>
+template <int GAP = 0, bool FEW = false, typename Args>
 __device__ __forceinline__ void dc_advance(const Args& a, DcWalk& w, int len) {
   w.t += len;
   w.page += len;
@@ -104,9 +109,9 @@ __device__ __forceinline__ void dc_advance(const Args& a, DcWalk& w, int len) {
       w.seq_first += a.n_kv * (w.np + GAP);
       w.b += 1;
       if (w.t < w.t_end) {
-        w.np = dc_pages<SINGLES>(a, w.b, &w.kv_len);
-        if constexpr (SINGLES)
-          while (w.np == 0 && w.b + 1 < a.n_seqs) w.np = dc_pages<SINGLES>(a, ++w.b, &w.kv_len);
+        w.np = dc_pages<FEW>(a, w.b, &w.kv_len);
+        if constexpr (FEW)
+          while (w.np == 0 && w.b + 1 < a.n_seqs) w.np = dc_pages<FEW>(a, ++w.b, &w.kv_len);
       }
     }
   }

@@ -284,6 +284,18 @@ def test_attend_chunk_that_fills_the_gpu(n_q, n_kv, dh):
         at += q[b]
 
 
+@pytest.mark.parametrize("n_q,n_kv,dh", [(4, 4, 128), (4, 2, 64), (3, 1, 96), (8, 2, 128), (5, 1, 64), (16, 2, 128), (16, 1, 64)])
+@pytest.mark.parametrize("q", [[1, 2, 3, 4, 5, 6, 7, 8, 9], [2, 2, 2, 2, 2, 2, 2, 2, 2], [1, 0, 4, 0, 2, 8, 1, 3, 300]])
+def test_attend_a_few_new_tokens(n_q, n_kv, dh, q):
+    """Around the number of tokens up to which a sequence goes the way of single tokens, at contexts whose pages end inside,
+    at and behind the new rows, and long enough to be split over CTAs."""
+    ctx = [0, 62, 63, 64, 60, 121, 2000, 5000, 127]
+    total = [a + b for a, b in zip(ctx, q)]
+    s = Setup(n_q, n_kv, dh, "e4m3", [max(t, 1) for t in total], seed=sum(q) + n_q)
+    s.fill(total, scale=1.5)
+    run_attend(s, ctx, q, scale=1.5, weights=True, window=2)
+
+
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
 @pytest.mark.parametrize("n_q,n_kv,dh", [(4, 2, 128), (3, 1, 96), (4, 4, 64)])
 def test_attend_long_chunks_beside_short_ones(fmt, n_q, n_kv, dh):
