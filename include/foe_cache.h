@@ -99,8 +99,9 @@ foe_status foe_cache_attend(foe_cache* cache, const void* q, long long q_stride,
  * whose scales are made anew from them; the pages the view names are not changed, so a page that sequences share can be a
  * source for all of them.  The pages of to_table are distinct and none of them is named by the view.
  * Results: new_lens [n_seqs] = min(tokens, budget); kept [n_seqs][n_kv_heads][budget] the kept positions; weights_out (or
- * NULL) [n_seqs][n_kv_heads], row stride weights_out_stride >= budget, the weights of the kept tokens, which must not
- * alias weights.  Entries and rows behind new_lens are left as they were.
+ * NULL) [n_seqs][n_kv_heads], row stride weights_out_stride >= budget, the weights of the kept tokens.  Entries and rows
+ * behind new_lens are left as they were.  Neither may weights_out be weights nor new_lens overlap the view's context_lens
+ * (FOE_ERR_UNSUPPORTED).
  * 0 <= sink, 0 <= recent, sink + recent <= budget, 64 * to_pages_per_seq >= budget >= 1 (FOE_ERR_SHAPE otherwise). */
 foe_status foe_cache_evict(foe_cache* cache, const foe_cache_view* view, const float* weights, long long weights_stride,
                            const int* to_table, int to_pages_per_seq, int budget, int sink, int recent, int* new_lens,

@@ -376,7 +376,9 @@ foe_status foe_cache_evict(foe_cache* h, const foe_cache_view* view, const float
   a.c = cache8_args(h, view, h->status);
   if (weights_stride < a.c.max_len || (weights_out && weights_out_stride < budget)) return FOE_ERR_SHAPE;
   if ((long long)view->n_seqs * ((budget + 63) / 64) >= (1LL << 31)) return FOE_ERR_SHAPE;
-  if (weights_out == weights) return FOE_ERR_UNSUPPORTED;
+  // (the blocks of a sequence's KV heads read its length while one of them writes the new one)
+  const long long apart = new_lens - view->context_lens;
+  if (weights_out == weights || (apart < view->n_seqs && -apart < view->n_seqs)) return FOE_ERR_UNSUPPORTED;
   if (!right_device(h)) return FOE_ERR_UNSUPPORTED;
   a.weights = weights; a.weights_stride = weights_stride; a.to_table = to_table; a.to_pages_per_seq = to_pages_per_seq;
   a.budget = budget; a.sink = sink; a.recent = recent; a.new_lens = new_lens; a.kept = kept;

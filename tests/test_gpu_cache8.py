@@ -474,6 +474,20 @@ def test_evict_shared_source_pages_and_nan_pages():
     run_evict(s, lens, 64, 1, 5)
 
 
+def test_evict_refuses_lengths_in_place():
+    """The blocks of the other KV heads read a sequence's length while new_lens is written."""
+    s = Setup(4, 4, 64, "e4m3", [200, 100], seed=77, extra_pages=2)
+    s.fill([200, 100])
+    lens = i32([200, 100, 0, 0])
+    view = s.pool.view(s.table.cuda(), lens[:2])
+    w, to = torch.rand(2, 4, s.width * PAGE, device="cuda"), s.spare[:2].view(2, 1).cuda()
+    kept = torch.zeros(2, 4, 64, dtype=torch.int32, device="cuda")
+    refused(-4, s.ops.evict, view, w, to, 64, 1, 3, lens[:2], kept)
+    refused(-4, s.ops.evict, view, w, to, 64, 1, 3, lens[1:3], kept)
+    s.ops.evict(view, w, to, 64, 1, 3, lens[2:], kept)
+    assert lens.tolist() == [200, 100, 64, 64]
+
+
 def test_evict_long_sequence():
     s = Setup(1, 1, 64, "e4m3", [70000], seed=22, extra_pages=20)
     s.fill([70000])
