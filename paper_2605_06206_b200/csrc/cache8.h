@@ -98,7 +98,7 @@ int cache8_chunk_max_split_blocks();
 size_t cache8_chunk_part_rows(int n_sms);
 cudaError_t cache8_chunk_configure();
 void launch_cache8_weights(int fmt, const Cache8WeightsArgs& w, int n_sms, cudaStream_t st);
-void launch_cache8_evict(int fmt, const Cache8EvictArgs& a, cudaStream_t st);
+void launch_cache8_evict(int fmt, const Cache8EvictArgs& a, int n_sms, cudaStream_t st);
 cudaError_t cache8_evict_configure();
 
 }  // namespace foe

@@ -386,7 +386,7 @@ foe_status foe_cache_evict(foe_cache* h, const foe_cache_view* view, const float
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   h->last_stream = st;
   g_overlap_launches = true;
-  launch_cache8_evict(h->cfg.format, a, st);
+  launch_cache8_evict(h->cfg.format, a, h->n_sms, st);
   return launched();
 }
 

@@ -1,16 +1,18 @@
 // Eviction from the 8-bit cache by accumulated attention weight: every (sequence, KV head) keeps its first `sink`
 // tokens, its last `recent` ones and the heaviest of the rest, budget tokens in all, in their order.
 //
-// Two launches.  The first chooses: one block per (sequence, KV head) finds the k-th largest weight by a radix search
-// over the weights as ordered integers (three passes of 11, 11 and 10 bits over keys in shared memory), then writes the
-// kept positions, each thread those of a run whose place a prefix sum gives; ties go to the lower position.  The second copies: one block per (destination page, KV
-// head, K or V) gathers its 64 rows, takes their largest magnitude and encodes them at a scale made for them.  Source and
+// The choice: one block per (sequence, KV head) finds the k-th largest weight by a radix search over the weights as ordered
+// integers (digits of 11, 11 and 10 bits over keys in shared memory, the first counted while they are read), then goes over
+// the positions 32 at a time, what stays of them as one word; ties go to the lower position.  The copy: 64 rows of a
+// destination page are gathered, their largest magnitude taken and encoded at a scale made for them.  Source and
 // destination pages are disjoint, so all destination pages are built at once, and a source page that several sequences
-// share (a common prompt prefix) is left as it is for the others.
+// share (a common prompt prefix) is left as it is for the others.  Calls whose pages fit the device do both in one launch
+// (cache8_cut_kernel), others in two.
 // Bound: memory (4 bytes per weight; 2 bytes read and 2 written per kept K/V element pair).  Measured (B200): 32 sequences of
-// 4k to 9k tokens, 8 KV heads of 128, cut to 2048: 69 us, 19 for the choice and 50 for the copy (5.3 TB/s); one sequence of
-// 1500 tokens 9.6 us.  Reading the weights again in every pass and scanning tile by tile took 34 us for the choice, decoding
-// every code to find the largest 73 us for the copy.
+// 4k to 9k tokens, 8 KV heads of 128, cut to 2048: 68 us, 18 for the choice and 50 for the copy (5.3 TB/s); one sequence of
+// 1500 tokens, 4 KV heads, cut to 512: 7.3 us (in two launches 8.2; with five barriers a digit and a thread's run of
+// positions at a time 9.7), of 40,000 tokens cut to 1024 24 us, most of it issuing instructions for the keys.  Counting the
+// first digit in two copies, by a lane's parity, made no difference.
 #include "cache8.cuh"
 #include "cache8.h"
 
@@ -18,7 +20,7 @@ namespace foe {
 
 constexpr int kEvThreads = 1024;
 constexpr int kEvBins = 2048;
-constexpr int kEvKeysMax = 48 * 1024;            // keys that fit the shared memory of one block, beside the bins
+constexpr int kEvKeysMax = 47 * 1024;            // keys that fit the shared memory of one block, beside the counts and pages
 
 // order of the weights as unsigned integers: larger weight, larger key; -0 = +0; a NaN below everything
 __device__ __forceinline__ uint32_t weight_key(float x) {
@@ -33,10 +35,162 @@ __device__ __forceinline__ float key_weight(uint32_t u) {
   return __uint_as_float(u == 0u ? 0x7fc00000u : ((u & 0x80000000u) ? (u & 0x7fffffffu) : ~u));
 }
 
-// sum of v over the threads before this one (every warp adds up the other warps' sums by itself)
-__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* warp_sums) {
-  static_assert(kEvThreads == 1024, "one warp sum per lane");
+constexpr int kEvWarps = kEvThreads / 32;
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+
+struct __align__(16) EvSmem {
+  uint32_t hist[3][kEvBins];                               // one for each digit, so that none is cleared between passes
+  uint32_t sums[3][kEvWarps];
+  uint32_t keep[kEvWarps], eq[kEvWarps];
+  uint32_t found[3][3];                                    // digit, keys in higher bins, keys in its bin
+};
+
+// Which of a row's positions stay: those outside [lo, hi), of the others the keys with (u & mask) > prefix and the first k
+// of those with (u & mask) == prefix.
+struct EvChoice {
+  int lo, hi;
+  uint32_t prefix, mask;
+  int k;
+};
+
+// (shared memory only: while the kernel before this one ends; a barrier stands before the first count)
+__device__ __forceinline__ void ev_clear(EvSmem& sm) {
+  uint4* h = reinterpret_cast<uint4*>(&sm.hist[0][0]);
+  for (int i = threadIdx.x; i < 3 * kEvBins / 4; i += kEvThreads) h[i] = make_uint4(0, 0, 0, 0);
+}
+
+// Reads the row's weights once, as keys, and counts the candidates' first digits on the way.
+__device__ __forceinline__ void ev_stage(const float* wt, int len, int lo, int hi, uint32_t* keys, EvSmem& sm) {
+  constexpr int AHEAD = 8;                                 // loads in flight
+  for (int j0 = threadIdx.x; j0 < len; j0 += AHEAD * kEvThreads) {
+    float x[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) x[i] = j0 + i * kEvThreads < len ? __ldg(wt + j0 + i * kEvThreads) : 0.f;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int j = j0 + i * kEvThreads;
+      const uint32_t u = weight_key(x[i]);
+      if (j < len) keys[j] = u;
+      if (j >= lo && j < hi) atomicAdd(&sm.hist[0][u >> 21], 1u);
+    }
+  }
+}
+
+// The want-th largest of key(lo .. hi - 1), 0 <= want < hi - lo, as a choice: a radix search over digits of 11, 11 and 10
+// bits that ends early where everything that shares the digits found so far stays.  COUNTED: the first digits are counted.
+// Barriers: before the first read of the counts (and of staged keys), at least one.
+template <bool COUNTED, typename Key>
+__device__ __forceinline__ EvChoice ev_choose(Key key, int lo, int hi, int want, EvSmem& sm) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  EvChoice ch = {lo, hi, 0u, 0u, 0};
+  if (want == 0) {                                         // no key is above all bits set, and none of the equal ones stays
+    ch.prefix = ch.mask = 0xffffffffu;
+    __syncthreads();
+    return ch;
+  }
+  ch.k = want;
+#pragma unroll 1
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0);
+    const uint32_t dmask = pass == 2 ? 1023u : 2047u;
+    uint32_t* hist = sm.hist[pass];
+    if (pass > 0 || !COUNTED) {
+#pragma unroll 4
+      for (int j = lo + tid; j < hi; j += kEvThreads) {
+        const uint32_t u = key(j);
+        // (adding up a warp's equal bins first, by match or by ballot, measured slower than the plain additions)
+        if ((u & ch.mask) == ch.prefix) atomicAdd(&hist[(u >> shift) & dmask], 1u);
+      }
+    }
+    __syncthreads();
+    // The digit whose bin holds the k-th largest.  Bins from the top down: rank r is bin kEvBins - 1 - r.  Every warp adds
+    // up 64 ranks; the first warp finds the warp whose ranks hold it and looks among those.
+    const uint32_t two = hist[kEvBins - 1 - (warp * 64 + lane)] + hist[kEvBins - 1 - (warp * 64 + 32 + lane)];
+    const uint32_t sum = __reduce_add_sync(0xffffffffu, two);
+    if (lane == 0) sm.sums[pass][warp] = sum;
+    __syncthreads();
+    if (warp == 0) {
+      auto scan = [lane](uint32_t x) {
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const uint32_t u = __shfl_up_sync(0xffffffffu, x, o);
+          if (lane >= o) x += u;
+        }
+        return x;
+      };
+      const uint32_t k = uint32_t(ch.k), mine = sm.sums[pass][lane], incl = scan(mine);
+      const int w = __ffs(__ballot_sync(0xffffffffu, incl >= k)) - 1;           // (want < hi - lo: there is one)
+      const uint32_t base = __shfl_sync(0xffffffffu, incl - mine, w);
+      const int top = kEvBins - 1 - (w * 64 + 2 * lane);                          // a lane's ranks: two neighbours
+      const uint32_t n0 = hist[top], n1 = hist[top - 1];
+      const uint32_t upto = base + scan(n0 + n1);
+      const int l = __ffs(__ballot_sync(0xffffffffu, upto >= k)) - 1;
+      if (lane == l) {
+        const uint32_t above = upto - n0 - n1;
+        const bool second = above + n0 < k;
+        sm.found[pass][0] = uint32_t(second ? top - 1 : top);
+        sm.found[pass][1] = second ? above + n0 : above;
+        sm.found[pass][2] = second ? n1 : n0;
+      }
+    }
+    __syncthreads();
+    ch.prefix |= sm.found[pass][0] << shift;
+    ch.mask |= dmask << shift;
+    ch.k -= int(sm.found[pass][1]);
+    if (int(sm.found[pass][2]) == ch.k) break;             // (the same in every thread)
+  }
+  return ch;
+}
+
+// emit(place, position, key) for each position of 0 .. len - 1 that stays and whose place is in [from, to).  A warp takes a
+// run of whole 32s: it counts what stays there, waits for the others' counts and goes over it again.  What stays of 32
+// positions is one word; 32 such words, one a lane, are a group.  KEPT: the words of the first sweep are held (rows of up to
+// kEvKeysMax tokens: two groups), otherwise they are made again.
+template <bool KEPT, typename Key, typename Emit>
+__device__ __forceinline__ void ev_keep(Key key, int len, const EvChoice& ch, EvSmem& sm, int from, int to, Emit emit) {
+  static_assert(kEvKeysMax <= 64 * kEvThreads, "two groups a warp");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int run = (len + kEvThreads - 1) / kEvThreads * 32;
+  const int j0 = min(warp * run, len), j1 = min(j0 + run, len);
+  // words of the group that starts at j: what stays whatever the ties do, and the ties
+  auto words = [&](int j, uint32_t& keep, uint32_t& tie) {
+    keep = tie = 0;
+    const int n = min(32, (j1 - j + 31) >> 5);
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+      const int at = j + i * 32 + lane;
+      const bool in = at < j1, forced = at < ch.lo || at >= ch.hi;
+      const uint32_t u = in ? key(at) & ch.mask : 0u;
+      const uint32_t kw = __ballot_sync(0xffffffffu, in && (forced || u > ch.prefix));
+      const uint32_t tw = __ballot_sync(0xffffffffu, in && !forced && u == ch.prefix);
+      if (lane == i) { keep = kw; tie = tw; }
+    }
+  };
+  uint32_t kw[2] = {0, 0}, tw[2] = {0, 0}, n_keep = 0, n_eq = 0;
+  if constexpr (KEPT) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      if (j0 + g * 1024 < j1) words(j0 + g * 1024, kw[g], tw[g]);
+      n_keep += __popc(kw[g]);
+      n_eq += __popc(tw[g]);
+    }
+  } else {
+    for (int j = j0; j < j1; j += 1024) {
+      words(j, kw[0], tw[0]);
+      n_keep += __popc(kw[0]);
+      n_eq += __popc(tw[0]);
+    }
+  }
+  n_keep = __reduce_add_sync(0xffffffffu, n_keep);
+  n_eq = __reduce_add_sync(0xffffffffu, n_eq);
+  if (lane == 0) { sm.keep[warp] = n_keep; sm.eq[warp] = n_eq; }
+  __syncthreads();
+  const uint32_t k = uint32_t(ch.k);
+  uint32_t eq = __reduce_add_sync(0xffffffffu, lane < warp ? sm.eq[lane] : 0u);         // ties before, of which k stay
+  int at = int(__reduce_add_sync(0xffffffffu, lane < warp ? sm.keep[lane] : 0u) + min(eq, k));
+  const uint32_t below = (1u << lane) - 1;
   auto scan = [lane](uint32_t x) {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -45,13 +199,42 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* warp_sums) 
     }
     return x;
   };
-  const uint32_t incl = scan(v);
-  __syncthreads();                                         // (the sums of an earlier scan have been read)
-  if (lane == 31) warp_sums[warp] = incl;
-  __syncthreads();
-  const uint32_t mine = warp_sums[lane];
-  const uint32_t before = scan(mine) - mine;
-  return __shfl_sync(0xffffffffu, before, warp) + incl - v;
+  auto write = [&](int j, uint32_t keep, uint32_t tie) {
+    if (__any_sync(0xffffffffu, tie != 0)) {               // the lowest ties that still fit join those that stay
+      const uint32_t upto = eq + scan(__popc(tie));
+      uint32_t rank = upto - __popc(tie);
+      for (uint32_t left = tie; left && rank < k; ++rank, left &= left - 1) keep |= left & -left;
+      eq = __shfl_sync(0xffffffffu, upto, 31);
+    }
+    const int n = __popc(keep), end = at + int(scan(n));
+    for (uint32_t need = __ballot_sync(0xffffffffu, n > 0 && end - n < to && end > from); need; need &= need - 1) {
+      const int i = __ffs(need) - 1;
+      const uint32_t w = __shfl_sync(0xffffffffu, keep, i);
+      const int mine = __shfl_sync(0xffffffffu, end - n, i) + __popc(w & below), pos = j + i * 32 + lane;
+      if (((w >> lane) & 1u) && mine >= from && mine < to) emit(mine, pos, key(pos));
+    }
+    at = __shfl_sync(0xffffffffu, end, 31);
+  };
+  if constexpr (KEPT) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+      if (j0 + g * 1024 < j1) write(j0 + g * 1024, kw[g], tw[g]);
+  } else {
+    for (int j = j0; j < j1; j += 1024) {
+      words(j, kw[0], tw[0]);
+      write(j, kw[0], tw[0]);
+    }
+  }
+}
+
+// tokens that sequence b holds; lengths out of range are reported and count as none
+__device__ __forceinline__ int ev_len(const Cache8Args& c, int b) {
+  int len = c.context_lens[b];
+  if (len < 0 || len > c.max_len) {
+    if (threadIdx.x == 0) atomicExch(c.status, kStatusBounds);
+    len = 0;
+  }
+  return len;
 }
 
 // STAGED: the row's keys are read once into shared memory (rows of up to kEvKeysMax tokens); otherwise every pass reads the
@@ -59,19 +242,15 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* warp_sums) 
 template <bool STAGED>
 __global__ void __launch_bounds__(kEvThreads)
 cache8_select_kernel(const Cache8EvictArgs a) {
+  extern __shared__ uint32_t keys[];
+  __shared__ EvSmem sm;
+  ev_clear(sm);
   pdl_wait();
   pdl_launch_dependents();
-  extern __shared__ uint32_t keys[];
-  __shared__ uint32_t hist[kEvBins];
-  __shared__ uint32_t warp_sums[kEvThreads / 32];
-  __shared__ uint32_t found[2];
+  __syncthreads();
   const Cache8Args& c = a.c;
-  const int b = blockIdx.y, kvh = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
-  int len = c.context_lens[b];
-  if (len < 0 || len > c.max_len) {
-    if (tid == 0) atomicExch(c.status, kStatusBounds);
-    len = 0;
-  }
+  const int b = blockIdx.y, kvh = blockIdx.x, tid = threadIdx.x;
+  const int len = ev_len(c, b);
   const size_t row = size_t(b) * c.n_kv + kvh;
   const float* wt = a.weights + row * a.weights_stride;
   int* kept = a.kept + row * a.budget;
@@ -87,99 +266,12 @@ cache8_select_kernel(const Cache8EvictArgs a) {
   const int lo = a.sink, hi = len - a.recent;              // the candidates
   const int want = a.budget - a.sink - a.recent;           // how many of them stay; 0 <= want < hi - lo
   auto key = [&](int j) { return STAGED ? keys[j] : weight_key(wt[j]); };
-  if (STAGED) {
-    constexpr int AHEAD = 8;                               // loads in flight
-    for (int j0 = tid; j0 < len; j0 += AHEAD * kEvThreads) {
-      float x[AHEAD];
-#pragma unroll
-      for (int i = 0; i < AHEAD; ++i) x[i] = j0 + i * kEvThreads < len ? __ldg(wt + j0 + i * kEvThreads) : 0.f;
-#pragma unroll
-      for (int i = 0; i < AHEAD; ++i)
-        if (j0 + i * kEvThreads < len) keys[j0 + i * kEvThreads] = weight_key(x[i]);
-    }
-  }
-  uint32_t prefix = 0, mask = 0;                           // digits of the want-th largest key found so far
-  int k = want;                                            // how many keys with these digits stay
-#pragma unroll 1
-  for (int pass = 0; pass < 3 && want > 0; ++pass) {
-    const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0);
-    const uint32_t dmask = pass == 2 ? 1023u : 2047u;
-    for (int i = tid; i < kEvBins; i += kEvThreads) hist[i] = 0;
-    __syncthreads();
-    for (int j = lo + tid; j < hi; j += kEvThreads) {
-      const uint32_t u = key(j);
-      // (adding up a warp's equal bins first, by match or by ballot, measured slower than the plain additions)
-      if ((u & mask) == prefix) atomicAdd(&hist[(u >> shift) & dmask], 1u);
-    }
-    __syncthreads();
-    // the digit whose bin holds the k-th largest: thread t sums its bins from the top down
-    constexpr int PER = kEvBins / kEvThreads;
-    uint32_t mine = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) mine += hist[kEvBins - 1 - (tid * PER + i)];
-    uint32_t above = block_scan(mine, warp_sums);     // keys in higher bins
-    if (above < uint32_t(k) && above + mine >= uint32_t(k)) {
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int bin = kEvBins - 1 - (tid * PER + i);
-        const uint32_t n = hist[bin];
-        if (above < uint32_t(k) && above + n >= uint32_t(k)) { found[0] = uint32_t(bin); found[1] = above; break; }
-        above += n;
-      }
-    }
-    __syncthreads();
-    prefix |= found[0] << shift;
-    mask |= dmask << shift;
-    k -= int(found[1]);
-  }
-  __syncthreads();                                         // (with want == 0: the staged keys are there)
-  // Keys above `prefix` stay, and the first k of those equal to it.  A thread takes a run of consecutive positions, its
-  // length odd so that the threads of a warp read different banks; one scan gives every run its place.
-  const int run = ((len + kEvThreads - 1) / kEvThreads) | 1;
-  const int j0 = min(tid * run, len), j1 = min(j0 + run, len);
-  if constexpr (STAGED) {
-    static_assert(kEvKeysMax / kEvThreads < 64, "a run's positions are the bits of one word");
-    unsigned long long keep = 0, eq = 0;                   // kept whatever the ties do; equal to the last one kept
-    for (int j = j0; j < j1; ++j) {
-      const uint32_t u = keys[j];
-      const bool forced = j < lo || j >= hi;
-      keep |= (unsigned long long)(forced || (want > 0 && u > prefix)) << (j - j0);
-      eq |= (unsigned long long)(!forced && want > 0 && u == prefix) << (j - j0);
-    }
-    uint32_t at = block_scan(__popcll(keep), warp_sums);
-    const uint32_t eq_before = block_scan(__popcll(eq), warp_sums);
-    at += min(eq_before, uint32_t(k));
-    for (uint32_t n = eq_before; eq && n < uint32_t(k); ++n, eq &= eq - 1) keep |= eq & -eq;      // the lowest ties that still fit
-    for (; keep; keep &= keep - 1, ++at) {
-      const int j = j0 + __ffsll(keep) - 1;
-      kept[at] = j;
-      if (wout) wout[at] = key_weight(keys[j]);
-    }
-    return;
-  }
-  uint32_t n_keep = 0, n_eq = 0;
-  for (int j = j0; j < j1; ++j) {
-    if (j < lo || j >= hi) { ++n_keep; continue; }
-    const uint32_t u = key(j);
-    n_keep += want > 0 && u > prefix;
-    n_eq += want > 0 && u == prefix;
-  }
-  uint32_t at = block_scan(n_keep, warp_sums);
-  uint32_t eq = block_scan(n_eq, warp_sums);
-  at += min(eq, uint32_t(k));
-  for (int j = j0; j < j1; ++j) {
-    bool keep = j < lo || j >= hi;
-    if (!keep && want > 0) {
-      const uint32_t u = key(j);
-      keep = u > prefix;
-      if (u == prefix) keep = eq++ < uint32_t(k);
-    }
-    if (keep) {
-      kept[at] = j;
-      if (wout) wout[at] = wt[j];
-      ++at;
-    }
-  }
+  if (STAGED) ev_stage(wt, len, lo, hi, keys, sm);
+  const EvChoice ch = ev_choose<STAGED>(key, lo, hi, want, sm);
+  ev_keep<STAGED>(key, len, ch, sm, 0, a.budget, [&](int at, int j, uint32_t u) {
+    kept[at] = j;
+    if (wout) wout[at] = STAGED ? key_weight(u) : wt[j];
+  });
 }
 
 // Largest magnitude of 16 codes, as a number.  e4m3 magnitudes are ordered like their codes without the sign; int8 codes
@@ -288,25 +380,164 @@ cache8_gather_kernel(const Cache8EvictArgs a) {
   if (threadIdx.x == 0) (is_v ? c.v_scales : c.k_scales)[to] = nan ? __int_as_float(0x7fc00000) : c8_pow2(e);
 }
 
-template <int FMT>
-static void launch_evict_t(const Cache8EvictArgs& a, cudaStream_t st) {
+// Choice and copy in one launch, for calls whose destination pages fit the device at kCutPages a CTA.  Block (part, kvh, b)
+// makes the pages [part * per, (part + 1) * per) of its pair: every part of a pair finds the whole choice by itself, beside
+// the others, and keeps the positions of its own pages in shared memory.  The row's page ids and scales are fetched while
+// the choice is made, so that between it and the copy stands no load but the rows' own.
+// Measured (B200, us as one launch / as two): 4 KV heads of 128, 1500 tokens to 512 7.3 / 8.2; 8 heads, 8000 to 1024
+// 11.0 / 12.1; at two pages a CTA 8 heads, 8000 to 2048 12.1 / 12.7, four sequences of 3000 to 512 10.2 / 11.1; at four
+// pages a CTA 8000 to 4096 14.0 / 13.8, four sequences of 3000 to 1024 12.4 / 12.3.
+constexpr int kCutPages = 2;
+template <int FMT, int DH>
+__global__ void __launch_bounds__(kEvThreads)
+cache8_cut_kernel(const Cache8EvictArgs a, int per) {
+  constexpr int CH = DH / 16;                              // 16-code pieces of a row
+  constexpr int T = 64 * CH;                               // threads for the K or the V rows of a page: one piece each
+  constexpr int GROUPS = kEvThreads / T;                   // of them at a time
+  constexpr int ITERS = (2 * kCutPages + GROUPS - 1) / GROUPS;
+  static_assert(T % 32 == 0 && T / 32 <= 32, "groups of whole warps");
+  extern __shared__ uint32_t keys[];
+  __shared__ EvSmem sm;
+  __shared__ int page_s[kEvKeysMax / 64];                  // the row's pages (-1: outside the pool) and their K and V scales
+  __shared__ float scale_s[2][kEvKeysMax / 64];
+  __shared__ int pos_s[kCutPages * 64];
+  __shared__ uint32_t red[ITERS][kEvThreads / 32];
+  ev_clear(sm);
+  pdl_wait();
+  pdl_launch_dependents();
+  __syncthreads();
   const Cache8Args& c = a.c;
-  if (c.max_len <= kEvKeysMax) launch_pdl(cache8_select_kernel<true>, dim3(c.n_kv, c.n_seqs), dim3(kEvThreads), size_t(c.max_len) * 4, st, a);
+  const int b = blockIdx.z, kvh = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int len = ev_len(c, b);
+  const int n = min(len, a.budget), first = int(blockIdx.x) * per * 64, mine = min(n - first, per * 64);
+  if (blockIdx.x == 0 && kvh == 0 && tid == 0) a.new_lens[b] = n;
+  if (mine <= 0) return;
+  const size_t row = size_t(b) * c.n_kv + kvh;
+  const float* wt = a.weights + row * a.weights_stride;
+  int* kept = a.kept + row * a.budget;
+  float* wout = a.weights_out ? a.weights_out + row * a.weights_out_stride : nullptr;
+  const int group = tid / T, p = tid - group * T;
+  const int n_units = (mine + 63) / 64 * 2;                // K and V of each page
+  int to_page[ITERS];
+#pragma unroll
+  for (int it = 0; it < ITERS; ++it) {
+    const int unit = it * GROUPS + group;
+    to_page[it] = -1;
+    if (group < GROUPS && unit < n_units) to_page[it] = a.to_table[size_t(b) * a.to_pages_per_seq + first / 64 + (unit >> 1)];
+  }
+  static_assert(kEvKeysMax / 64 <= kEvThreads, "a thread per page");
+  int page = -1;
+  if (tid < (len + 63) >> 6) page = c.block_table[size_t(b) * c.max_pages_per_seq + tid];
+  const bool cut = len > a.budget;
+  const int lo = a.sink, hi = len - a.recent;              // the candidates of a cut
+  const int want = a.budget - a.sink - a.recent;           // how many of them stay; 0 <= want < hi - lo
+  if (cut) ev_stage(wt, len, lo, hi, keys, sm);
+  if (tid < (len + 63) >> 6) {                             // (the scales arrive while the choice is made)
+    const bool ok = page >= 0 && page < c.num_pages;
+    page_s[tid] = ok ? page : -1;
+    if (ok) {
+      cp_async4(smem_u32(&scale_s[0][tid]), c.k_scales + page * c.n_kv + kvh);
+      cp_async4(smem_u32(&scale_s[1][tid]), c.v_scales + page * c.n_kv + kvh);
+    } else {
+      scale_s[0][tid] = scale_s[1][tid] = 0.f;
+    }
+  }
+  auto emit = [&](int at, int j, float w) {
+    pos_s[at - first] = j;
+    kept[at] = j;
+    if (wout) wout[at] = w;
+  };
+  if (cut) {
+    auto key = [&](int j) { return keys[j]; };
+    const EvChoice ch = ev_choose<true>(key, lo, hi, want, sm);
+    ev_keep<true>(key, len, ch, sm, first, first + mine, [&](int at, int j, uint32_t u) { emit(at, j, key_weight(u)); });
+  } else {
+    for (int j = first + tid; j < first + mine; j += kEvThreads) emit(j, j, wout ? wt[j] : 0.f);
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();
+  const int r = p / CH, ch = p - r * CH;
+  uint4 x[ITERS];
+  float scale[ITERS];
+  bool bad = false;
+#pragma unroll
+  for (int it = 0; it < ITERS; ++it) {
+    const int unit = it * GROUPS + group, at = (unit >> 1) * 64 + r, is_v = unit & 1;
+    x[it] = make_uint4(0, 0, 0, 0);
+    scale[it] = 0.f;
+    if (group < GROUPS && at < mine) {                     // (so unit < n_units)
+      const int pos = pos_s[at], pg = page_s[pos >> 6];
+      scale[it] = scale_s[is_v][pos >> 6];
+      if (pg >= 0) x[it] = *reinterpret_cast<const uint4*>((is_v ? c.v_pages : c.k_pages) + ((size_t(pg) * c.n_kv + kvh) * 64 + (pos & 63)) * DH + ch * 16);
+      else bad = true;
+    }
+    if (it * GROUPS >= n_units) continue;
+    // fp32 bits of the largest magnitude; a NaN scale wins
+    const uint32_t amax = __reduce_max_sync(0xffffffffu, __float_as_uint(largest_of<FMT>(x[it]) * scale[it]) & 0x7fffffffu);
+    if (lane == 0) red[it][warp] = amax;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int it = 0; it < ITERS; ++it) {
+    const int unit = it * GROUPS + group, at = (unit >> 1) * 64 + r, is_v = unit & 1;
+    if (group >= GROUPS || unit >= n_units) break;         // (the same for a whole warp)
+    const uint32_t amax = __reduce_max_sync(0xffffffffu, lane < T / 32 ? red[it][group * (T / 32) + lane] : 0u);
+    if (to_page[it] < 0 || to_page[it] >= c.num_pages) { bad = true; continue; }
+    const int e = c8_exponent<FMT>(amax >> 16);            // (values held in 8 bits have at most 8 significant ones)
+    const bool nan = e == 0x7fffffff;
+    const size_t to = size_t(to_page[it]) * c.n_kv + kvh;
+    if (at < mine) {                                       // rows behind the last kept one stay as they were
+      const float f = scale[it] * (nan ? 0.f : c8_pow2(-e));
+      uint4 v = x[it];
+      if (nan) v = make_uint4(0, 0, 0, 0);
+      else if (f != 1.f) v = make_uint4(c8_rescale4<FMT>(v.x, f), c8_rescale4<FMT>(v.y, f), c8_rescale4<FMT>(v.z, f), c8_rescale4<FMT>(v.w, f));
+      reinterpret_cast<uint4*>((is_v ? c.v_pages : c.k_pages) + to * 64 * DH)[p] = v;
+    }
+    if (p == 0) (is_v ? c.v_scales : c.k_scales)[to] = nan ? __int_as_float(0x7fc00000) : c8_pow2(e);
+  }
+  if (bad) atomicExch(c.status, kStatusBounds);
+}
+
+template <int FMT, int DH>
+static void launch_evict_dh(const Cache8EvictArgs& a, int n_sms, cudaStream_t st) {
+  const Cache8Args& c = a.c;
+  const int blocks = (a.budget + 63) / 64;
+  const size_t smem = size_t(c.max_len) * 4;
+  // one launch if some number of pages a CTA lets every CTA have an SM
+  for (int per = 1; per <= kCutPages && c.max_len <= kEvKeysMax; ++per) {
+    const int parts = (blocks + per - 1) / per;
+    if ((long long)parts * c.n_kv * c.n_seqs > n_sms) continue;
+    launch_pdl(cache8_cut_kernel<FMT, DH>, dim3(parts, c.n_kv, c.n_seqs), dim3(kEvThreads), smem, st, a, per);
+    return;
+  }
+  if (c.max_len <= kEvKeysMax) launch_pdl(cache8_select_kernel<true>, dim3(c.n_kv, c.n_seqs), dim3(kEvThreads), smem, st, a);
   else launch_pdl(cache8_select_kernel<false>, dim3(c.n_kv, c.n_seqs), dim3(kEvThreads), 0, st, a);
-  const dim3 grid(unsigned(c.n_seqs) * ((a.budget + 63) / 64), c.n_kv, 2);
-  if (c.dh == 64) launch_pdl(cache8_gather_kernel<FMT, 64>, grid, dim3(kGaThreads), 0, st, a);
-  else if (c.dh == 96) launch_pdl(cache8_gather_kernel<FMT, 96>, grid, dim3(kGaThreads), 0, st, a);
-  else launch_pdl(cache8_gather_kernel<FMT, 128>, grid, dim3(kGaThreads), 0, st, a);
+  launch_pdl(cache8_gather_kernel<FMT, DH>, dim3(unsigned(c.n_seqs) * blocks, c.n_kv, 2), dim3(kGaThreads), 0, st, a);
+}
+
+template <int FMT>
+static void launch_evict_t(const Cache8EvictArgs& a, int n_sms, cudaStream_t st) {
+  if (a.c.dh == 64) launch_evict_dh<FMT, 64>(a, n_sms, st);
+  else if (a.c.dh == 96) launch_evict_dh<FMT, 96>(a, n_sms, st);
+  else launch_evict_dh<FMT, 128>(a, n_sms, st);
 }
 
 cudaError_t cache8_evict_configure() {
-  return cudaFuncSetAttribute(cache8_select_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvKeysMax * 4);
+  const void* kernels[] = {(const void*)cache8_select_kernel<true>, (const void*)cache8_cut_kernel<kC8E4M3, 64>,
+                           (const void*)cache8_cut_kernel<kC8E4M3, 96>, (const void*)cache8_cut_kernel<kC8E4M3, 128>,
+                           (const void*)cache8_cut_kernel<kC8Int8, 64>, (const void*)cache8_cut_kernel<kC8Int8, 96>,
+                           (const void*)cache8_cut_kernel<kC8Int8, 128>};
+  for (const void* k : kernels) {
+    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvKeysMax * 4);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
 }
 
-void launch_cache8_evict(int fmt, const Cache8EvictArgs& a, cudaStream_t st) {
+void launch_cache8_evict(int fmt, const Cache8EvictArgs& a, int n_sms, cudaStream_t st) {
   if (a.c.n_seqs <= 0) return;
-  if (fmt == kC8E4M3) launch_evict_t<kC8E4M3>(a, st);
-  else launch_evict_t<kC8Int8>(a, st);
+  if (fmt == kC8E4M3) launch_evict_t<kC8E4M3>(a, n_sms, st);
+  else launch_evict_t<kC8Int8>(a, n_sms, st);
 }
 
 }  // namespace foe

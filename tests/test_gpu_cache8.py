@@ -474,6 +474,52 @@ def test_evict_shared_source_pages_and_nan_pages():
     run_evict(s, lens, 64, 1, 5)
 
 
+@pytest.mark.parametrize("fmt,n_kv,dh", [("e4m3", 8, 128), ("int8", 8, 96), ("e4m3", 8, 64)])
+@pytest.mark.parametrize("budget", [256, 300, 512, 520, 1000])
+def test_evict_one_to_many_pages_a_block(fmt, n_kv, dh, budget):
+    """128 to 512 destination pages and K and V of each: one page a CTA, two, and a launch of its own for the copy."""
+    lens = [1300, 513, 700, 255]
+    s = Setup(n_kv, n_kv, dh, fmt, lens, seed=budget + dh, extra_pages=len(lens) * ((budget + 63) // 64))
+    s.fill(lens, k=s.randn(sum(lens), n_kv, dh) * torch.exp2((torch.arange(sum(lens)) % 9 - 4).float())[:, None, None].to(torch.bfloat16))
+    run_evict(s, lens, budget, 3, 60)
+
+
+@pytest.mark.parametrize("n,budget", [(40000, 640), (48128, 130), (48129, 130), (33000, 33000)])
+def test_evict_of_long_sequences_with_ties(n, budget):
+    """Around the longest row whose keys are held in shared memory; most weights equal, so that positions decide."""
+    s = Setup(2, 2, 64, "int8", [n], seed=n, extra_pages=(budget + 63) // 64)
+    s.fill([n])
+    w = (torch.rand(1, 2, s.width * PAGE, generator=s.g) * 1.003).floor()
+    run_evict(s, [n], budget, 2, 64, weights=w)
+
+
+@pytest.mark.parametrize("budget", [100, 1000])
+def test_evict_reports_pages_outside_the_pool(budget):
+    """A source page and a destination page that are not in the pool: reported, and nothing else of the pool changes."""
+    lens = [1100, 1100, 1100, 1100]
+    width = (budget + 63) // 64
+    s = Setup(8, 8, 64, "e4m3", lens, seed=78, extra_pages=len(lens) * width)
+    s.fill(lens)
+    to = s.spare[:4 * width].view(4, width).clone()
+    kept = torch.zeros(4, 8, budget, dtype=torch.int32, device="cuda")
+    w = torch.rand(4, 8, s.width * PAGE, device="cuda")
+    before = [t.clone() for t in (s.pool.k_pages, s.pool.v_pages)]
+    for what in ("source", "destination"):
+        bad = to.clone()
+        if what == "source":
+            s.table[1, 3] = s.num_pages
+        else:
+            s.table[1, 3] = 0
+            bad[2, 0] = -1
+        s.ops.evict(s.view(lens), w, bad.cuda(), budget, 1, 20, i32([0] * 4), kept)
+        assert s.ops.poll_status() == -8
+        assert s.ops.poll_status() == 0
+    spare = set(to.flatten().tolist())
+    others = torch.tensor([p for p in range(s.num_pages) if p not in spare], device="cuda")
+    for t, b in zip((s.pool.k_pages, s.pool.v_pages), before):
+        assert torch.equal(t[others], b[others])
+
+
 def test_evict_refuses_lengths_in_place():
     """The blocks of the other KV heads read a sequence's length while new_lens is written."""
     s = Setup(4, 4, 64, "e4m3", [200, 100], seed=77, extra_pages=2)
