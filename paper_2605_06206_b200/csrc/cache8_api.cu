@@ -180,7 +180,8 @@ int cache8_attend(foe_cache* h, const foe_cache_view* v, const void* q, long lon
     if (h->ws.pages && a.c.n_tokens > 0 && !make_query_map(&tmQ, q, a.c.n_tokens, a.c.n_q, a.c.dh, q_stride, q_head_stride)) return -1;
     // Sequences with a few new tokens go the way of single tokens: a tile of 128 query rows would read their cache at a
     // fraction of the memory's rate (16 query heads on 4 of 128; us as chunks / here: 2 new tokens at 16 x 8000 cached tokens
-    // 169 / 36, at 64 x 4000 340 / 58, at 64 x 500 69 / 22, at 1 x 8000 24.5 / 16.8).  (No sequence has fewer tokens than those that the others, at max_q_len each, leave.)
+    // 169 / 36, at 64 x 4000 340 / 58, at 64 x 500 69 / 22, at 1 x 8000 24.5 / 16.8).  No sequence has fewer tokens than
+    // those that the others, at max_q_len each, leave.
     const bool few = a.c.n_tokens - (long long)(a.c.n_seqs - 1) * a.c.max_q_len <= a.c.few_q;
     n = 0;
     if (few && a.c.n_tokens > 0) {

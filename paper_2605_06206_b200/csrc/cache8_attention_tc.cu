@@ -7,18 +7,19 @@
 //   * K and V pages arrive as codes (TMA, half the bytes) and four converter warps turn them into fp16 operand tiles
 //     in the 128-byte-swizzled layout, exactly and unscaled.  The page's K scale multiplies the scores and its V scale
 //     enters the exponent, t = s + log2(scale_v); the row sum takes it back out.
-//   * Q becomes fp16 once per CTA (long chunks, whose K tiles are expanded to bf16 beforehand, keep it as it is): a power of two per row brings the row's largest element to [2^7, 2^8), which keeps
-//     every bf16 value within 2^31 of it (the factor joins the K scale).  P is fp16 too (11 bits where bf16 has 8),
+//   * Q becomes fp16 once per CTA (long chunks, whose K tiles are expanded to bf16 beforehand, keep it as it is): a power of
+//     two per row brings the row's largest element to [2^7, 2^8), which keeps every bf16 value within 2^31 of it (the
+//     factor joins the K scale).  P is fp16 too (11 bits where bf16 has 8),
 //     kept 2^6 above its natural scale so that only probabilities below 2^-30 of the largest are lost.
 //   * K and V tiles have rings of their own: a K tile is free as soon as its scores exist, so the converters run ahead.
 //   * Calls with few query blocks split their keys over CTAs, as evenly as the call's lengths allow; each split leaves
 //     (m, l, unnormalised O) and a second kernel joins them in order.
 // Bound: the chain of a step (scores -> maximum -> exponentials -> P V) of two tiles, as in the bf16 kernel: tensor pipe 52 %
 // active, special-function unit 53 %.  Measured (B200): four prompts of 4096 tokens, 16 query and 4 KV heads of 128, e4m3:
-// 260 us with the 10 us that expand the pages (1.06 PFLOP/s; every block converting its own 367, the bf16 kernel on a bf16
-// cache 240); three chunks of 300 to 600 tokens over 3k to 16k, 8 and 4 heads of 64, int8: 81 us and 12 to join.
-// Warp roles (768 threads; 640 on expanded tiles, which have no converters): warp 0 TMA producer, warps 1 and 2 MMA issuers (one per head), warps 4-7 converters, warps
-// 8-23 softmax.
+// 254 us with the 10 us that expand the pages (1.08 PFLOP/s; every block converting its own 367, the bf16 kernel on a bf16
+// cache 240); three chunks of 300 to 600 tokens over 3k to 16k, 8 and 4 heads of 64, int8: 79 us, 11 to expand and 11 to join.
+// Warp roles (768 threads; 640 on expanded tiles, which have no converters): warp 0 TMA producer, warps 1 and 2 MMA issuers
+// (one per head), warps 4-7 converters, warps 8-23 softmax.
 #include <math.h>
 
 #include "attention_tc.cuh"
