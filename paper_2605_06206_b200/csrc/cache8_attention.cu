@@ -365,8 +365,13 @@ cache8_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         for (int n = 0; n < NT; ++n) {
           const float r0 = (m_ref[n][0] == -INFINITY ? 0.f : m_ref[n][0]) - kD8Shift, r1 = (m_ref[n][1] == -INFINITY ? 0.f : m_ref[n][1]) - kD8Shift;
           const float p0 = fast_exp2(s[n][0] - r0), p1 = fast_exp2(s[n][1] - r1), p2 = fast_exp2(s[n][2] - r0), p3 = fast_exp2(s[n][3] - r1);
-          l_run[n][0] = fmaf(p0 + p2, sc.z, l_run[n][0]);
-          l_run[n][1] = fmaf(p1 + p3, sc.z, l_run[n][1]);
+          float z0 = sc.z, z1 = sc.z;
+          if (tail) {                                              // (a page that the row does not see may have a NaN scale)
+            if (p0 + p2 == 0.f) z0 = 0.f;
+            if (p1 + p3 == 0.f) z1 = 0.f;
+          }
+          l_run[n][0] = fmaf(p0 + p2, z0, l_run[n][0]);
+          l_run[n][1] = fmaf(p1 + p3, z1, l_run[n][1]);
           pb[n][0] = movmatrix_trans(pack_f16(p0, p1));
           pb[n][1] = movmatrix_trans(pack_f16(p2, p3));
         }

@@ -488,7 +488,7 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         tmem_ld32(s_base, r0);                               // two loads in flight, one wait
         tmem_ld32(s_base + 32, r1);
         const float4 sc4 = scales[j % kC8Scales];
-        const float sc = rf * sc4.x;
+        float sc = rf * sc4.x, sv_log2 = sc4.y, sv_inv = sc4.z;
         tmem_ld_wait();
         tc_fence_before();                                   // the scores are in registers: the buffer may take step j+1
         __syncwarp();
@@ -500,6 +500,7 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             if (k0 + i > qpos) r0[i] = 0xff800000u;          // -inf: key after the query
             if (k0 + 32 + i > qpos) r1[i] = 0xff800000u;
           }
+          if (k0 > qpos) { sc = 1.f; sv_log2 = sv_inv = 0.f; }       // a page the row does not see: its scales may be NaN
         }
         float mx;
         {                                                    // four independent chains, then a short tree
@@ -512,7 +513,7 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           }
           mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
         }
-        const float m_new = fmaxf(m_ref, fmaf(mx, sc, sc4.y));
+        const float m_new = fmaxf(m_ref, fmaf(mx, sc, sv_log2));
         // move the reference maximum (and rescale O) only when it is off by more than 2^8; warp-uniform so that
         // the tensor-memory accesses stay aligned
         const bool move = __any_sync(0xffffffffu, m_new > m_ref + 8.0f);
@@ -542,7 +543,7 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           l_run *= alpha;
           m_ref = m_new;
         }
-        const float off = sc4.y + kC8Shift - ((m_ref == -INFINITY) ? 0.f : m_ref);
+        const float off = sv_log2 + kC8Shift - ((m_ref == -INFINITY) ? 0.f : m_ref);
         // probabilities, written as the fp16 A operand of the PV product (exp2(-inf) = 0 handles the mask)
         const uint32_t p_addr = p_base + (j & 1) * 32;
         if (j >= 2 && !mbar_wait(&o_full[2 * t + ph], ((j - 2) >> 1) & 1)) { ok = false; break; }   // P V of step j-2 has read this buffer
@@ -570,7 +571,7 @@ cache8_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         }
         float sum0, sum1;
         unpack_f32x2(add_f32x2(rs2[0], rs2[1]), sum0, sum1);
-        l_run = fmaf(sum0 + sum1, sc4.z, l_run);
+        l_run = fmaf(sum0 + sum1, sv_inv, l_run);
         if (!o_seen && !mbar_wait(&o_full[2 * t + (ph ^ 1)], ((j - 1) >> 1) & 1)) { ok = false; break; }
         tmem_st_wait();                                      // P is in tensor memory
         tc_fence_before();

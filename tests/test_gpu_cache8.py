@@ -406,6 +406,25 @@ def test_attend_shared_pages():
     run_attend(s, [120, 120], [8, 20], weights=True)
 
 
+@pytest.mark.parametrize("which", ["k", "v"])
+@pytest.mark.parametrize("fmt,n_q,n_kv,dh", [("e4m3", 4, 2, 128), ("int8", 8, 4, 64), ("e4m3", 8, 2, 96)])
+@pytest.mark.parametrize("ctx,q", [(62, 4), (63, 2), (60, 8), (0, 70), (30, 200), (2500, 100), (37, 2500)])
+def test_attend_nan_page_behind_a_row(fmt, n_q, n_kv, dh, ctx, q, which):
+    """The last page's scale is NaN: rows before it are what they are without, to the bit, the others NaN in that head."""
+    s = Setup(n_q, n_kv, dh, fmt, [ctx + q], seed=ctx + q)
+    s.fill([ctx + q])
+    x, view = s.randn(q, n_q, dh).cuda(), s.view([ctx], [q])
+    w = torch.zeros(1, n_kv, s.width * PAGE, device="cuda")
+    clean = s.ops.attend(x, view)
+    page = (ctx + q - 1) // PAGE
+    (s.pool.k_scales if which == "k" else s.pool.v_scales)[s.table[0, page].item(), 0] = math.nan
+    out = s.ops.attend(x, view, weights_in=w, weights_out=w)
+    assert s.ops.poll_status() == 0
+    first, group = page * PAGE - ctx, n_q // n_kv
+    assert first > 0 and torch.equal(out[:first], clean[:first]) and torch.equal(out[:, group:], clean[:, group:])
+    assert bool(out[first:, :group].isnan().all()) and bool(w[:, 1:, :ctx + q].isfinite().all())
+
+
 # ======================================================================================= eviction
 def run_evict(s, lens, budget, sink, recent, weights=None):
     n, width = len(lens), (budget + PAGE - 1) // PAGE
