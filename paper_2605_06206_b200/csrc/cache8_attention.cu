@@ -1,5 +1,5 @@
 // Attention of single new tokens over the 8-bit cache (in a call of chunks: of its sequences with up to few_q new tokens,
-// whose (query, head) rows of a KV head fit one tile of 8).
+// whose (query, head) rows of a KV head fit one tile of 8, or two where that is all the call has).
 //
 // Decode reads every code of the cache once: 1 byte per K and V element, so the kernel has half the time per element of
 // a bf16 one and its arithmetic has to be lean.
@@ -43,7 +43,7 @@ constexpr int kD8Parts = 80;                     // a pair is cut into about thi
 constexpr float kD8Shift = 6.f;                  // P' = 2^(t - m + shift)
 constexpr float kD8Lazy = 8.f;                   // the reference maximum moves when a score exceeds it by more than this
 
-template <int NT> struct D8Cfg {                 // NT: tiles of 8 heads
+template <int NT> struct D8Cfg {                 // NT: tiles of 8 rows
   static constexpr int kWarps = 4;               // consumers, each 16 keys of every page
   static constexpr int kCtas = NT == 1 ? 3 : 2;  // per SM (16 heads need twice the registers)
   static constexpr int kThreads = (kWarps + 1) * 32;
@@ -602,7 +602,7 @@ static void launch_decode_t(const CUtensorMap& tmK, const CUtensorMap& tmV, cons
 
 template <int FMT>
 static void launch_decode_format(const CUtensorMap& tmK, const CUtensorMap& tmV, const Cache8AttendArgs& a, int n_sms, cudaStream_t st) {
-  const bool wide = a.c.n_q / a.c.n_kv > 8;
+  const bool wide = a.c.n_q / a.c.n_kv * (a.c.q_lens ? a.c.few_q : 1) > 8;
   if (a.c.dh > 64) wide ? launch_decode_t<FMT, 128, 2>(tmK, tmV, a, n_sms, st) : launch_decode_t<FMT, 128, 1>(tmK, tmV, a, n_sms, st);
   else wide ? launch_decode_t<FMT, 64, 2>(tmK, tmV, a, n_sms, st) : launch_decode_t<FMT, 64, 1>(tmK, tmV, a, n_sms, st);
 }

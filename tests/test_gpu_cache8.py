@@ -285,7 +285,9 @@ def test_attend_chunk_that_fills_the_gpu(n_q, n_kv, dh):
 
 
 @pytest.mark.parametrize("n_q,n_kv,dh", [(4, 4, 128), (4, 2, 64), (3, 1, 96), (8, 2, 128), (5, 1, 64), (16, 2, 128), (16, 1, 64)])
-@pytest.mark.parametrize("q", [[1, 2, 3, 4, 5, 6, 7, 8, 9], [2, 2, 2, 2, 2, 2, 2, 2, 2], [1, 0, 4, 0, 2, 8, 1, 3, 300]])
+@pytest.mark.parametrize("q", [[1, 2, 3, 4, 5, 6, 7, 8, 9], [2, 2, 2, 2, 2, 2, 2, 2, 2], [1, 0, 4, 0, 2, 8, 1, 3, 300],
+                               [4, 3, 2, 4, 4, 1, 4, 0, 3], [8, 7, 6, 5, 8, 4, 3, 8, 1], [16, 1, 9, 15, 16, 12, 10, 16, 16],
+                               [3, 5, 4, 5, 5, 2, 5, 4, 3]])
 def test_attend_a_few_new_tokens(n_q, n_kv, dh, q):
     """Around the number of tokens up to which a sequence goes the way of single tokens, at contexts whose pages end inside,
     at and behind the new rows, and long enough to be split over CTAs."""
